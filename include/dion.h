@@ -276,6 +276,95 @@ int dion_shard_factor(dion_ctx* ctx, const dion_matrix* a, int64_t n_total, cons
 int dion_shard_finish(dion_ctx* ctx, const dion_matrix* a, int64_t n_total, const float* U, const float* W,
                       const float* colsumsq, const int* flag, float lr, void* cuda_stream);
 
+/* ---- calls over lists of arrays: what a training step needs around the Dion step ----------------------------------------
+ *
+ * dion_grad_norm   the global norm of a list of gradients (and the norm of each)
+ * dion_clip_grads  the list scaled by min(1, max_norm / norm)
+ * dion_adamw_step, dion_lion_step   the update of the parameters that are not matrices: norm gains, biases, embeddings
+ *
+ * A list is a HOST array of descriptors holding DEVICE pointers, read before the call returns; one call takes any number of
+ * arrays of any sizes and types in one launch per 250 (AdamW, Lion), 400 (scaling) or 500 (norm) of them.  An array is
+ * rows x cols with a leading dimension in elements (a vector is one row; rows or cols may be 0).  Pointers need the alignment
+ * of their element type only.
+ *
+ * Nothing that a call writes may be touched twice by it: neither the same array twice in a list nor overlapping ones
+ * (DION_ERR_ALIAS); column slices of one matrix do not overlap.  dion_grad_norm takes an array twice and counts it twice.
+ * The calls are asynchronous on `cuda_stream`, allocate nothing, leave the calling thread's current device as it was and may
+ * be captured into a CUDA graph (the host values of the call, lr and step among them, are those of the capture).
+ * Results do not depend on timing: the same call gives the same bits. */
+typedef enum { DION_NORM_2 = 0, DION_NORM_INF = 1 } dion_norm;
+
+typedef struct {
+  int64_t rows, cols;
+  const void* G;        /* g_dtype, rows x cols                                             */
+  int64_t ldg;          /* >= cols                                                          */
+  int g_dtype;          /* dion_dtype                                                       */
+  void* out;            /* dion_clip_grads: the result, of out_dtype; may be G itself (same */
+  int64_t ldo;          /* type and leading dimension).  dion_grad_norm ignores it.         */
+  int out_dtype;
+} dion_grad;
+
+/* Norm of all elements of the list: the 2-norm or the largest magnitude.  Sums are held in 64 bits, so neither large nor small
+ * gradients overflow or vanish in their squares.  Outputs are DEVICE floats, each optional but not all three NULL:
+ *   norm_out   the norm (0 of an empty list)
+ *   each_out   `count` norms, one per array
+ *   coef_out   min(1, max_norm / norm), what dion_clip_grads would multiply by, for dion_rule.grad_scale (max_norm >= 0, may be
+ *              infinite; ignored without coef_out)
+ * A norm that is not finite sets DION_STATUS_NONFINITE, and the coefficient is NaN. */
+int dion_grad_norm(dion_ctx* ctx, const dion_grad* list, int count, int norm_type, float max_norm, float* norm_out,
+                   float* each_out, float* coef_out, void* cuda_stream);
+
+/* out <- min(1, max_norm / norm) * G for every array of the list, one coefficient for all of it.
+ *   norms == NULL (num_norms 0): the norm is that of the list.
+ *   norms != NULL: DEVICE, num_norms floats: the norms of the parts (lists, or the shards of other ranks) whose whole is clipped;
+ *                  the norm is the norm of these norms.  The list itself is then read once only, and may be empty.
+ * norm_out, coef_out: optional DEVICE floats, the norm and the coefficient.  Arrays in place are left alone where the
+ * coefficient is 1.  A norm that is not finite sets DION_STATUS_NONFINITE and makes the coefficient, and so every result,
+ * NaN: dion_step cancels a step on such a gradient, dion_adamw_step and dion_lion_step one with such a grad_scale (a
+ * Lazy-Dion step between two refreshes does not look at its gradient: look at the status first). */
+int dion_clip_grads(dion_ctx* ctx, const dion_grad* list, int count, float max_norm, int norm_type, const float* norms,
+                    int num_norms, float* norm_out, float* coef_out, void* cuda_stream);
+
+/* A parameter that is updated element by element, and its state. */
+typedef struct {
+  int64_t rows, cols;
+  void* X;              /* fp32, in/out                                                     */
+  int64_t ldx;
+  const void* G;        /* g_dtype, read only                                               */
+  int64_t ldg;
+  int g_dtype;          /* dion_dtype                                                       */
+  void* M;              /* m_dtype, in/out: the (first) moment                              */
+  int64_t ldm;
+  int m_dtype;          /* dion_dtype; a bf16 moment is rounded to nearest when it is kept, */
+                        /* the step itself uses it unrounded                                */
+  void* V;              /* fp32, in/out: AdamW's second moment; dion_lion_step ignores it   */
+  int64_t ldv;
+  void* X16;            /* optional: bf16, receives the new X rounded to nearest            */
+  int64_t ldx16;
+  float lr_scale;       /* the learning rate of this parameter is lr * lr_scale             */
+  float weight_decay;   /* decoupled: X is first multiplied by 1 - lr * lr_scale * weight_decay */
+} dion_param;
+
+typedef struct {
+  double beta1, beta2;  /* in [0, 1)                                                        */
+  double eps;           /* AdamW: >= 0                                                      */
+  int64_t step;         /* AdamW: the number t of this step, from 1                         */
+  const int64_t* step_dev;  /* optional, AdamW: DEVICE, holds t instead of `step` (for captured steps; a step with t < 1 is
+                           cancelled)                                                       */
+  const float* grad_scale;  /* optional: DEVICE, the factor s of the gradients (a clipping coefficient).  One that is not finite
+                           cancels the step of the whole list: nothing is written, DION_STATUS_NONFINITE is set and the step
+                           counted as skipped (dion_get_status).                            */
+} dion_rule;
+
+/* One AdamW step on a list of parameters:  g = s G,  M <- beta1 M + (1 - beta1) g,  V <- beta2 V + (1 - beta2) g^2,
+ * X <- (1 - lr wd) X - lr (M / (1 - beta1^t)) / (sqrt(V / (1 - beta2^t)) + eps), lr being lr * lr_scale.  The arithmetic is
+ * fp32.  A NaN or Inf in G stays in its element. */
+int dion_adamw_step(dion_ctx* ctx, const dion_param* list, int count, const dion_rule* rule, float lr, void* cuda_stream);
+
+/* One Lion step:  g = s G,  X <- (1 - lr wd) X - lr sign(beta1 M + (1 - beta1) g),  M <- beta2 M + (1 - beta2) g, with
+ * sign(0) = 0 and the sign that of the exact sum. */
+int dion_lion_step(dion_ctx* ctx, const dion_param* list, int count, const dion_rule* rule, float lr, void* cuda_stream);
+
 /* Synchronises `cuda_stream`, then reports and clears the latched device status
  * (DION_STATUS_* bits) and the number of steps skipped because of a breakdown
  * since the last call.  Either output pointer may be NULL. */

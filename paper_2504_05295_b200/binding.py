@@ -20,13 +20,15 @@ DION_F32, DION_BF16 = 0, 1
 PREC_FP32, PREC_BF16_OPERANDS = 0, 1
 ORTH_AUTO, ORTH_CHOLQR2, ORTH_SHIFTED3, ORTH_HOUSEHOLDER, ORTH_RCQR = 0, 1, 2, 3, 4
 ENGINE_AUTO, ENGINE_SIMT, ENGINE_TENSOR = 0, 1, 2
+NORM_2, NORM_INF = 0, 1
 STATUS_BREAKDOWN, STATUS_NONFINITE, STATUS_TIMEOUT, STATUS_ILLCOND = 1, 2, 4, 8
 
 EXPORTS = ["dion_default_config", "dion_init", "dion_step", "dion_step_grouped", "dion_lazy_step",
            "dion_workspace_bytes", "dion_get_status", "dion_launch_count", "dion_destroy",
            "dion_strerror", "dion_profile_enable", "dion_profile_read", "dion_get_orth_rounds", "dion_get_fallbacks",
            "dion_step_noalloc", "dion_noalloc_scratch_limit", "dion_dp_project", "dion_dp_factor",
-           "dion_dp_finish", "dion_shard_project", "dion_orthonormalize", "dion_shard_factor", "dion_shard_finish"]
+           "dion_dp_finish", "dion_shard_project", "dion_orthonormalize", "dion_shard_factor", "dion_shard_finish",
+           "dion_grad_norm", "dion_clip_grads", "dion_adamw_step", "dion_lion_step"]
 PHASES = ["P", "ORTH", "R", "EF", "COLNORM", "X", "ORTH_GEMM"]
 
 
@@ -44,6 +46,27 @@ class DionMatrix(ctypes.Structure):
                 ("Q", ctypes.c_void_p), ("ldq", ctypes.c_int64),
                 ("colnorm_out", ctypes.c_void_p), ("transposed", ctypes.c_int),
                 ("sketch", ctypes.c_void_p), ("sketch_rows", ctypes.c_int64), ("ld_sketch", ctypes.c_int64)]
+
+
+class DionGrad(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("G", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("g_dtype", ctypes.c_int),
+                ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64), ("out_dtype", ctypes.c_int)]
+
+
+class DionParam(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("X", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("G", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("g_dtype", ctypes.c_int),
+                ("M", ctypes.c_void_p), ("ldm", ctypes.c_int64), ("m_dtype", ctypes.c_int),
+                ("V", ctypes.c_void_p), ("ldv", ctypes.c_int64),
+                ("X16", ctypes.c_void_p), ("ldx16", ctypes.c_int64),
+                ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float)]
+
+
+class DionRule(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("step", ctypes.c_int64), ("step_dev", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p)]
 
 
 class DionError(RuntimeError):
@@ -107,6 +130,14 @@ def load_library() -> ctypes.CDLL:
     lib.dion_shard_factor.restype = ci
     lib.dion_shard_finish.argtypes = [vp, ctypes.POINTER(DionMatrix), i64, vp, vp, vp, vp, f32, vp]
     lib.dion_shard_finish.restype = ci
+    lib.dion_grad_norm.argtypes = [vp, ctypes.POINTER(DionGrad), ci, ci, f32, vp, vp, vp, vp]
+    lib.dion_grad_norm.restype = ci
+    lib.dion_clip_grads.argtypes = [vp, ctypes.POINTER(DionGrad), ci, f32, ci, vp, ci, vp, vp, vp]
+    lib.dion_clip_grads.restype = ci
+    lib.dion_adamw_step.argtypes = [vp, ctypes.POINTER(DionParam), ci, ctypes.POINTER(DionRule), f32, vp]
+    lib.dion_adamw_step.restype = ci
+    lib.dion_lion_step.argtypes = [vp, ctypes.POINTER(DionParam), ci, ctypes.POINTER(DionRule), f32, vp]
+    lib.dion_lion_step.restype = ci
     lib.dion_destroy.argtypes = [vp]
     lib.dion_destroy.restype = None
     lib.dion_strerror.argtypes = [ci]
@@ -122,6 +153,12 @@ def strerror(code: int) -> str:
 def _check(code: int) -> None:
     if code != 0:
         raise DionError(code, strerror(code))
+
+
+def _norm_type(kind) -> int:
+    if str(kind) not in ("2", "2.0", "inf"):
+        raise ValueError("norm_type must be 2 or inf")
+    return NORM_INF if str(kind) == "inf" else NORM_2
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -172,6 +209,106 @@ def matrix_desc(X: torch.Tensor, M: torch.Tensor, G: torch.Tensor, Q: torch.Tens
     else:
         d.sketch, d.sketch_rows, d.ld_sketch = None, 0, 0
     return d
+
+
+# ---- lists of arrays: gradients to be clipped, parameters that are not matrices -----------------------------------
+
+_DTYPES = {torch.float32: DION_F32, torch.bfloat16: DION_BF16}
+
+
+def _layout(tensors):
+    """(rows, cols, leading dimensions) of tensors of one shape as the C-ABI sees them: one row where all are dense, else
+    the rows of 2-D tensors with unit column stride (a strided vector is one column)."""
+    shape = tensors[0].shape
+    if any(t.shape != shape for t in tensors):
+        raise ValueError("the tensors of one entry must have the same shape")
+    n = tensors[0].numel()
+    if all(t.is_contiguous() for t in tensors):
+        return 1, n, [n] * len(tensors)
+    if n == 0:
+        return 0, 0, [0] * len(tensors)
+    if len(shape) == 1:
+        return n, 1, [t.stride(0) for t in tensors]
+    if len(shape) != 2:
+        raise ValueError("tensors of more than two dimensions must be contiguous")
+    rows, cols = shape
+    if any(t.stride(1) != 1 and cols > 1 for t in tensors):
+        raise ValueError("matrices must have unit column stride")
+    return rows, cols, [t.stride(0) if rows > 1 else cols for t in tensors]
+
+
+class _List:
+    """Packed descriptors for the calls over lists.  Holds the tensors, so that their memory lives as long as the list."""
+
+    def __init__(self, descs, kind, tensors):
+        self.arr, self.count = (kind * len(descs))(*descs), len(descs)
+        self.tensors = tuple(tensors)
+        devices = {t.device for t in self.tensors}
+        if len(devices) > 1:
+            raise ValueError("the tensors of a list must be on one device")
+        self.device = next(iter(devices)).index if devices else None
+
+    def __len__(self):
+        return self.count
+
+
+class GradList(_List):
+    pass
+
+
+class ParamList(_List):
+    pass
+
+
+def _cuda(**tensors):
+    for name, t in tensors.items():
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+
+
+def grad_list(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None) -> GradList:
+    """Describes gradients for ``Dion.grad_norm`` and ``Dion.clip_grads``: float32 or bfloat16 CUDA tensors of any shape,
+    contiguous or 2-D with unit column stride.  outs: where the clipped gradients go (same shapes, float32 or bfloat16);
+    without it they are clipped in place.  To be made again when a tensor is replaced."""
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    if len(outs) != len(grads):
+        raise ValueError("as many outs as grads")
+    descs = []
+    for G, out in zip(grads, outs):
+        _cuda(G=G, out=out)
+        if G.dtype not in _DTYPES or out.dtype not in _DTYPES:
+            raise ValueError("gradients must be float32 or bfloat16")
+        rows, cols, (ldg, ldo) = _layout([G, out])
+        descs.append(DionGrad(rows, cols, G.data_ptr(), ldg, _DTYPES[G.dtype], out.data_ptr(), ldo, _DTYPES[out.dtype]))
+    return GradList(descs, DionGrad, grads + outs)
+
+
+def param_desc(X: torch.Tensor, G: torch.Tensor, M: torch.Tensor, V: Optional[torch.Tensor] = None,
+               X16: Optional[torch.Tensor] = None, lr_scale: float = 1.0, weight_decay: float = 0.0):
+    """One parameter for ``param_list``: X float32, G and M float32 or bfloat16, V float32 (AdamW's second moment; Lion needs
+    none), X16 an optional bfloat16 copy of X to be kept up to date.  Equal shapes; contiguous, or 2-D with unit column stride."""
+    tensors = {"X": X, "G": G, "M": M, "V": V, "X16": X16}
+    given = {k: t for k, t in tensors.items() if t is not None}
+    _cuda(**given)
+    if X.dtype != torch.float32 or (V is not None and V.dtype != torch.float32):
+        raise ValueError("X and V must be float32")
+    if G.dtype not in _DTYPES or M.dtype not in _DTYPES:
+        raise ValueError("G and M must be float32 or bfloat16")
+    if X16 is not None and X16.dtype != torch.bfloat16:
+        raise ValueError("X16 must be bfloat16")
+    rows, cols, lds = _layout(list(given.values()))
+    ld = dict(zip(given, lds))
+    ptr = lambda k: tensors[k].data_ptr() if tensors[k] is not None else None  # noqa: E731
+    desc = DionParam(rows, cols, ptr("X"), ld["X"], ptr("G"), ld["G"], _DTYPES[G.dtype], ptr("M"), ld["M"], _DTYPES[M.dtype],
+                     ptr("V"), ld.get("V", 0), ptr("X16"), ld.get("X16", 0), float(lr_scale), float(weight_decay))
+    return desc, tuple(given.values())
+
+
+def param_list(params: Iterable) -> ParamList:
+    """Packs what ``param_desc`` returned, for ``Dion.adamw_step`` and ``Dion.lion_step``."""
+    params = list(params)
+    return ParamList([d for d, _ in params], DionParam, [t for _, ts in params for t in ts])
 
 
 def step_noalloc(X, M, G, Q, lr: float, mu: float = 0.95, eps: float = 1e-8, colnorm_out=None,
@@ -268,6 +405,63 @@ class Dion:
                      flag: torch.Tensor, lr: float, stream=None) -> None:
         _check(self._lib.dion_shard_finish(self._ctx, ctypes.byref(desc), int(n_total), U.data_ptr(), W.data_ptr(),
                                            colsumsq.data_ptr(), flag.data_ptr(), float(lr), _stream_ptr(stream)))
+
+    # calls over lists of arrays
+    def _list_call(self, items, kind, stream, floats):
+        """Stream and output pointers of a call over a list."""
+        if not isinstance(items, kind):
+            raise TypeError(f"expected a {kind.__name__}")
+        if items.device is not None and items.device != self.device:
+            raise ValueError("the list's tensors are not on the context's device")
+        ptrs = []
+        for name, t, least in floats:
+            if t is not None and (not t.is_cuda or t.device.index != self.device or t.dtype != torch.float32
+                                  or t.numel() < least or not t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous float32 tensor of >= {least} elements on the context's device")
+            ptrs.append(t.data_ptr() if t is not None and t.numel() else None)
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        return int(stream.cuda_stream), ptrs
+
+    def grad_norm(self, grads: GradList, norm_type=2, norm_out: Optional[torch.Tensor] = None,
+                  each_out: Optional[torch.Tensor] = None, max_norm: float = float("inf"),
+                  coef_out: Optional[torch.Tensor] = None, stream=None) -> None:
+        """The global norm of a list into ``norm_out`` (1 float32), the norm of every tensor into ``each_out`` and the
+        clipping coefficient min(1, max_norm / norm) into ``coef_out``: at least one of them.  norm_type: 2 or inf."""
+        st, (norm, each, coef) = self._list_call(grads, GradList, stream, (("norm_out", norm_out, 1), ("each_out", each_out, grads.count),
+                                                                          ("coef_out", coef_out, 1)))
+        _check(self._lib.dion_grad_norm(self._ctx, grads.arr, grads.count, _norm_type(norm_type), float(max_norm), norm, each, coef, st))
+
+    def clip_grads(self, grads: GradList, max_norm: float, norms: Optional[torch.Tensor] = None, norm_type=2,
+                   norm_out: Optional[torch.Tensor] = None, coef_out: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Scales a list by min(1, max_norm / norm), the norm being that of the list or, where ``norms`` is given, that of the
+        norms in it (of several lists, or of every rank's shard)."""
+        st, (parts, norm, coef) = self._list_call(grads, GradList, stream, (("norms", norms, 1), ("norm_out", norm_out, 1),
+                                                                           ("coef_out", coef_out, 1)))
+        _check(self._lib.dion_clip_grads(self._ctx, grads.arr, grads.count, float(max_norm), _norm_type(norm_type), parts,
+                                         norms.numel() if norms is not None else 0, norm, coef, st))
+
+    def adamw_step(self, params: ParamList, lr: float, step, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8,
+                   grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+        """One AdamW step on a list.  step: its number t, from 1, or an int64 CUDA tensor that holds it.  grad_scale: the
+        factor of the gradients on the device (a clipping coefficient)."""
+        st, (scale,) = self._list_call(params, ParamList, stream, (("grad_scale", grad_scale, 1),))
+        t_host, t_dev = 0, None
+        if isinstance(step, torch.Tensor):
+            if not step.is_cuda or step.device.index != self.device or step.dtype != torch.int64 or step.numel() != 1:
+                raise ValueError("step must be a number or an int64 tensor of one element on the context's device")
+            t_dev = step.data_ptr()
+        else:
+            t_host = int(step)
+        rule = DionRule(beta1, beta2, eps, t_host, t_dev, scale)
+        _check(self._lib.dion_adamw_step(self._ctx, params.arr, params.count, ctypes.byref(rule), float(lr), st))
+
+    def lion_step(self, params: ParamList, lr: float, beta1: float = 0.95, beta2: float = 0.98,
+                  grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+        """One Lion step on a list (``adamw_step``)."""
+        st, (scale,) = self._list_call(params, ParamList, stream, (("grad_scale", grad_scale, 1),))
+        rule = DionRule(beta1, beta2, 0.0, 1, None, scale)
+        _check(self._lib.dion_lion_step(self._ctx, params.arr, params.count, ctypes.byref(rule), float(lr), st))
 
     def lazy_step_desc(self, desc: DionMatrix, lr: float, refresh: bool, stream_ptr: int) -> None:
         _check(self._lib.dion_lazy_step(self._ctx, ctypes.byref(desc), float(lr), int(bool(refresh)), stream_ptr))

@@ -17,7 +17,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdion_b200.so")
 OBJ_DIR = os.path.join(HERE, "_obj")
-SOURCES = ["dion_api.cu", "umma_gemm.cu"]
+SOURCES = ["dion_api.cu", "umma_gemm.cu", "list_ops.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

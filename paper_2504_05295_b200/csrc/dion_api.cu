@@ -14,6 +14,7 @@
 #include "colnorm.cuh"
 #include "dion_common.cuh"
 #include "dion_internal.h"
+#include "list_api.cuh"
 #include "orth_kernels.cuh"
 #include "simt_gemm.cuh"
 #include "umma_api.cuh"
@@ -111,6 +112,7 @@ struct dion_ctx {
   int flag_cursor;
   int* flow_ctl = nullptr;   // progress counters of k_chol_flow (zero between launches)
   i64 flow_ctl_cap = 0;
+  void* list_scratch = nullptr;   // partial sums of the calls over lists
   int64_t launches;
   // per-phase profiling (off by default)
   bool prof_on;
@@ -2584,13 +2586,15 @@ int dion_init(dion_ctx** out, const dion_config* cfg) {
   c->cfg = *cfg;
   c->sm_count = prop.multiProcessorCount;
   void* p = nullptr;
-  constexpr size_t int_bytes = sizeof(int) * (8 + MAX_FLAG_SLOTS * OS_SLOT_INTS + 24 + FLOW_CTL_INTS);
+  constexpr size_t ctl_bytes = (sizeof(int) * (8 + MAX_FLAG_SLOTS * OS_SLOT_INTS + 24 + FLOW_CTL_INTS) + 127) / 128 * 128;
+  const size_t int_bytes = ctl_bytes + list::scratch_bytes(c->sm_count);
   if (cudaMalloc(&p, int_bytes) != cudaSuccess) { delete c; return DION_ERR_NOMEM; }
   c->dev_ints = (int*)p;
   c->flow_ctl = c->dev_ints + 8 + MAX_FLAG_SLOTS * OS_SLOT_INTS + 24;      // (128-byte aligned)
   c->flow_ctl_cap = FLOW_CTL_INTS;
+  c->list_scratch = (char*)p + ctl_bytes;
   if (cudaMemset(p, 0, int_bytes) != cudaSuccess) { cudaFree(p); delete c; return DION_ERR_CUDA; }
-  if (configure_kernels() != DION_OK) { cudaFree(p); delete c; return DION_ERR_CUDA; }
+  if (configure_kernels() != DION_OK || list::configure() != DION_OK) { cudaFree(p); delete c; return DION_ERR_CUDA; }
   if (cudaStreamCreateWithFlags(&c->side, cudaStreamNonBlocking) != cudaSuccess) { cudaGetLastError(); c->side = nullptr; }
   // graph replay of small steps: a capture stream and the scalars the graphs read; off if either cannot be had
   umma::pair_clusters(c->sm_count);      // (asked once per device, outside any capture)
@@ -2938,6 +2942,62 @@ int dion_shard_finish(dion_ctx* ctx, const dion_matrix* a, int64_t n_total, cons
     DION_TRY(x_update(s, 0, a, U, r, (const float*)a->Q, a->ldq, s.ws + s.L.P1, s.ws + s.L.R, alpha, flag));
   }
   return DION_OK;
+}
+
+// ---- calls over lists of arrays (list_ops.cu) -----------------------------------------------
+
+namespace {
+
+// The context's device for the time of a call.
+struct OnDevice {
+  int before = -1;
+  bool ok;
+  explicit OnDevice(int device) {
+    ok = cudaGetDevice(&before) == cudaSuccess && (before == device || cudaSetDevice(device) == cudaSuccess);
+    if (!ok) cudaGetLastError();
+    if (before == device) before = -1;
+  }
+  ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
+};
+
+list::Where list_call(dion_ctx* c, void* cuda_stream) {
+  return {c->sm_count, c->list_scratch, c->dev_ints, &c->launches, (cudaStream_t)cuda_stream};
+}
+
+}  // namespace
+
+int dion_grad_norm(dion_ctx* ctx, const dion_grad* list, int count, int norm_type, float max_norm, float* norm_out,
+                   float* each_out, float* coef_out, void* cuda_stream) {
+  DION_TRY(list::check_norm(list, count, norm_type, max_norm, norm_out, each_out, coef_out));
+  if (ctx == nullptr) return DION_ERR_INVALID;
+  const OnDevice on(ctx->cfg.device);
+  if (!on.ok) return DION_ERR_CUDA;
+  return list::grad_norm(list_call(ctx, cuda_stream), list, count, norm_type, max_norm, norm_out, each_out, coef_out);
+}
+
+int dion_clip_grads(dion_ctx* ctx, const dion_grad* list, int count, float max_norm, int norm_type, const float* norms,
+                    int num_norms, float* norm_out, float* coef_out, void* cuda_stream) {
+  DION_TRY(list::check_clip(list, count, max_norm, norm_type, norms, num_norms, norm_out, coef_out));
+  if (ctx == nullptr) return DION_ERR_INVALID;
+  const OnDevice on(ctx->cfg.device);
+  if (!on.ok) return DION_ERR_CUDA;
+  return list::clip_grads(list_call(ctx, cuda_stream), list, count, max_norm, norm_type, norms, num_norms, norm_out, coef_out);
+}
+
+int dion_adamw_step(dion_ctx* ctx, const dion_param* list, int count, const dion_rule* rule, float lr, void* cuda_stream) {
+  DION_TRY(list::check_step(true, list, count, rule, lr));
+  if (ctx == nullptr) return DION_ERR_INVALID;
+  const OnDevice on(ctx->cfg.device);
+  if (!on.ok) return DION_ERR_CUDA;
+  return list::param_step(list_call(ctx, cuda_stream), true, list, count, rule, lr);
+}
+
+int dion_lion_step(dion_ctx* ctx, const dion_param* list, int count, const dion_rule* rule, float lr, void* cuda_stream) {
+  DION_TRY(list::check_step(false, list, count, rule, lr));
+  if (ctx == nullptr) return DION_ERR_INVALID;
+  const OnDevice on(ctx->cfg.device);
+  if (!on.ok) return DION_ERR_CUDA;
+  return list::param_step(list_call(ctx, cuda_stream), false, list, count, rule, lr);
 }
 
 int dion_get_status(dion_ctx* ctx, void* cuda_stream, int* device_status, int* steps_skipped) {

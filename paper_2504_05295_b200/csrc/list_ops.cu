@@ -1,0 +1,338 @@
+// Calls over lists of arrays: argument checks, the launches' descriptor tables, launches.
+#include <math.h>
+#include <stdlib.h>
+#include <string.h>
+#include <algorithm>
+#include <new>
+
+#include "list_api.cuh"
+#include "list_kernels.cuh"
+
+namespace dion {
+namespace list {
+
+namespace {
+
+constexpr int BLOCKS_PER_SM = 8;
+// Arrays in one launch: its parameters end at 32764 bytes.  Small lists take small parameters.
+constexpr int FEW = 24;
+constexpr int MANY_NORM = 500, MANY_SCALE = 400, MANY_STEP = 250;
+constexpr i64 MAX_ELEMENTS = (i64)1 << 50;      // (no element count or byte offset overflows)
+
+template <typename... KArgs, typename... Args>
+int launch(const Where& w, void (*kernel)(KArgs...), i64 tiles, const Args&... args) {
+  i64 blocks = (i64)w.sm_count * BLOCKS_PER_SM;
+  if (blocks > tiles) blocks = tiles;
+  if (blocks < 1) blocks = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(THREADS); cfg.stream = w.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  ++*w.launches;
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) { cudaGetLastError(); return DION_ERR_CUDA; }
+  return DION_OK;
+}
+
+inline int bytes_of(int dtype) { return dtype == DION_BF16 ? 2 : 4; }
+inline bool known_type(int dtype) { return dtype == DION_F32 || dtype == DION_BF16; }
+
+// rows x cols elements, or a refusal
+int check_shape(i64 rows, i64 cols) {
+  if (rows < 0 || cols < 0 || rows > MAX_ELEMENTS || cols > MAX_ELEMENTS) return DION_ERR_SHAPE;
+  return cols != 0 && rows > MAX_ELEMENTS / cols ? DION_ERR_SHAPE : DION_OK;
+}
+int check_array(const void* p, i64 rows, i64 cols, i64 ld, int size) {
+  if (rows == 0 || cols == 0) return DION_OK;
+  if (p == nullptr) return DION_ERR_INVALID;
+  if (ld < cols || (rows > 1 && ld > MAX_ELEMENTS / rows)) return DION_ERR_SHAPE;
+  return (uintptr_t)p & (uintptr_t)(size - 1) ? DION_ERR_ALIGN : DION_OK;
+}
+
+// Memory that a call reads or writes.  Rows of `width` bytes, `pitch` bytes apart.
+struct Range {
+  uintptr_t begin, end;
+  uintptr_t width, pitch;      // pitch 0: one row
+  bool written;
+};
+Range range_of(const void* p, i64 rows, i64 cols, i64 ld, int size, bool written) {
+  Range r;
+  r.begin = (uintptr_t)p;
+  r.width = (uintptr_t)(cols * size);
+  r.pitch = rows > 1 && ld != cols ? (uintptr_t)(ld * size) : 0;
+  if (r.pitch == 0) r.width = (uintptr_t)(rows * cols * size);
+  r.end = r.begin + (r.pitch == 0 ? r.width : (uintptr_t)(rows - 1) * r.pitch + r.width);
+  r.written = written;
+  return r;
+}
+bool conflict(const Range& a, const Range& b) {
+  if ((!a.written && !b.written) || a.begin >= b.end || b.begin >= a.end) return false;
+  if (a.pitch != 0 && a.pitch == b.pitch) {      // two column slices of one matrix
+    const Range &lo = a.begin <= b.begin ? a : b, &hi = a.begin <= b.begin ? b : a;
+    const uintptr_t off = (hi.begin - lo.begin) % a.pitch;
+    return !(off >= lo.width && off + hi.width <= a.pitch);
+  }
+  return true;
+}
+
+// Whether anything that the call writes is touched twice.  Lists are often views of a few buffers: ranges that come in
+// ascending order need no sorting.
+int check_ranges(Range* r, size_t n) {
+  const auto before = [](const Range& a, const Range& b) { return a.begin < b.begin; };
+  if (!std::is_sorted(r, r + n, before)) std::sort(r, r + n, before);
+  for (size_t i = 0; i < n; ++i)
+    for (size_t j = i + 1; j < n && r[j].begin < r[i].end; ++j)
+      if (conflict(r[i], r[j])) return DION_ERR_ALIAS;
+  return DION_OK;
+}
+
+struct Ranges {
+  Range* r;
+  size_t n = 0;
+  explicit Ranges(size_t most) : r(new (std::nothrow) Range[most]) {}
+  ~Ranges() { delete[] r; }
+  Ranges(const Ranges&) = delete;
+  Ranges& operator=(const Ranges&) = delete;
+  void add(const void* p, i64 rows, i64 cols, i64 ld, int size, bool written) {
+    if (p != nullptr && rows > 0 && cols > 0) r[n++] = range_of(p, rows, cols, ld, size, written);
+  }
+};
+
+bool norm_type_ok(int t) { return t == DION_NORM_2 || t == DION_NORM_INF; }
+
+int check_floats(const float* p) { return (uintptr_t)p & 3 ? DION_ERR_ALIGN : DION_OK; }
+
+#define LIST_TRY(expr)              \
+  do {                              \
+    const int rc_ = (expr);         \
+    if (rc_ != DION_OK) return rc_; \
+  } while (0)
+
+// Dense arrays are one row.
+void flatten(i64 rows, i64 cols, bool dense, i64* n, i64* row) {
+  *n = rows * cols;
+  *row = dense || rows == 1 ? *n : cols;
+  if (*row < 1) *row = 1;
+}
+
+template <class Item, int CAP>
+i64 add_tiles(Table<Item, CAP>* t, Item* it) {
+  it->first = t->tiles;
+  t->tiles += (it->n + TILE - 1) / TILE;
+  return t->tiles;
+}
+
+template <int CAP>
+int norm_launches(const Where& w, const dion_grad* list, int count, bool inf, NormOut o, float* each) {
+  Table<NormItem, CAP> t;
+  int done = 0;
+  do {
+    t.tiles = 0;
+    t.count = std::min(count - done, CAP);
+    for (int i = 0; i < t.count; ++i) {
+      const dion_grad& a = list[done + i];
+      NormItem* it = &t.item[i];
+      it->g = a.G; it->g_bf16 = a.g_dtype == DION_BF16; it->ldg = a.ldg;
+      flatten(a.rows, a.cols, a.ldg == a.cols, &it->n, &it->cols);
+      add_tiles(&t, it);
+    }
+    o.each = each != nullptr ? each + done : nullptr;
+    o.use_carry = done > 0;
+    o.last = done + t.count == count;
+    done += t.count;
+    if (inf) LIST_TRY(launch(w, k_list_norm<CAP, true>, t.tiles, t, o));
+    else LIST_TRY(launch(w, k_list_norm<CAP, false>, t.tiles, t, o));
+  } while (done < count);
+  return DION_OK;
+}
+
+template <int CAP>
+int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
+  Table<ScaleItem, CAP> t;
+  int done = 0;
+  do {
+    t.tiles = 0;
+    t.count = std::min(count - done, CAP);
+    for (int i = 0; i < t.count; ++i) {
+      const dion_grad& a = list[done + i];
+      ScaleItem* it = &t.item[i];
+      it->g = a.G; it->g_bf16 = a.g_dtype == DION_BF16; it->ldg = a.ldg;
+      it->out = a.out; it->o_bf16 = a.out_dtype == DION_BF16; it->ldo = a.ldo;
+      flatten(a.rows, a.cols, a.ldg == a.cols && a.ldo == a.cols, &it->n, &it->cols);
+      add_tiles(&t, it);
+    }
+    done += t.count;
+    LIST_TRY(launch(w, k_list_scale<CAP>, t.tiles, t, c));
+    c.norm_out = nullptr; c.coef_out = nullptr;
+  } while (done < count);
+  return DION_OK;
+}
+
+template <int CAP, bool ADAMW>
+int step_launches(const Where& w, const dion_param* list, int count, Rule r, float lr) {
+  Table<StepItem, CAP> t;
+  int done = 0;
+  while (done < count) {
+    t.tiles = 0;
+    t.count = std::min(count - done, CAP);
+    for (int i = 0; i < t.count; ++i) {
+      const dion_param& a = list[done + i];
+      StepItem* it = &t.item[i];
+      it->X = (float*)a.X; it->ldx = a.ldx;
+      it->G = a.G; it->ldg = a.ldg; it->g_bf16 = a.g_dtype == DION_BF16;
+      it->M = a.M; it->ldm = a.ldm; it->m_bf16 = a.m_dtype == DION_BF16;
+      it->V = ADAMW ? (float*)a.V : nullptr; it->ldv = a.ldv;
+      it->X16 = (__nv_bfloat16*)a.X16; it->ldx16 = a.ldx16;
+      it->lr = lr * a.lr_scale;
+      it->keep = (float)(1.0 - (double)lr * a.lr_scale * a.weight_decay);
+      flatten(a.rows, a.cols, a.ldx == a.cols && a.ldg == a.cols && a.ldm == a.cols && (!ADAMW || a.ldv == a.cols) &&
+                              (a.X16 == nullptr || a.ldx16 == a.cols), &it->n, &it->cols);
+      add_tiles(&t, it);
+    }
+    r.first = done == 0;
+    done += t.count;
+    LIST_TRY(launch(w, k_list_step<CAP, ADAMW>, t.tiles, t, r));
+  }
+  return DION_OK;
+}
+
+template <typename K>
+bool load(K kernel) {
+  cudaFuncAttributes fa;
+  if (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess) { cudaGetLastError(); return false; }
+  return true;
+}
+
+}  // namespace
+
+size_t scratch_bytes(int sm_count) { return sizeof(Scratch) + sizeof(double) * ((size_t)sm_count * BLOCKS_PER_SM + MANY_NORM); }
+
+int configure() {
+  const bool ok = load(k_list_norm<FEW, false>) && load(k_list_norm<FEW, true>) && load(k_list_norm<MANY_NORM, false>) &&
+                  load(k_list_norm<MANY_NORM, true>) && load(k_list_scale<FEW>) && load(k_list_scale<MANY_SCALE>) &&
+                  load(k_list_step<FEW, false>) && load(k_list_step<FEW, true>) && load(k_list_step<MANY_STEP, false>) &&
+                  load(k_list_step<MANY_STEP, true>);
+  return ok ? DION_OK : DION_ERR_CUDA;
+}
+
+int check_norm(const dion_grad* list, int count, int norm_type, float max_norm, const float* norm_out, const float* each_out, const float* coef_out) {
+  if (count < 0 || (count > 0 && list == nullptr) || !norm_type_ok(norm_type)) return DION_ERR_INVALID;
+  if (norm_out == nullptr && each_out == nullptr && coef_out == nullptr) return DION_ERR_INVALID;
+  if (coef_out != nullptr && !(max_norm >= 0.f)) return DION_ERR_INVALID;
+  LIST_TRY(check_floats(norm_out));
+  LIST_TRY(check_floats(each_out));
+  LIST_TRY(check_floats(coef_out));
+  Ranges ranges((size_t)count + 3);
+  if (ranges.r == nullptr) return DION_ERR_NOMEM;
+  for (int i = 0; i < count; ++i) {
+    const dion_grad& a = list[i];
+    if (!known_type(a.g_dtype)) return DION_ERR_INVALID;
+    LIST_TRY(check_shape(a.rows, a.cols));
+    LIST_TRY(check_array(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype)));
+    ranges.add(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype), false);
+  }
+  ranges.add(norm_out, 1, 1, 1, 4, true);
+  ranges.add(each_out, 1, count, count, 4, true);
+  ranges.add(coef_out, 1, 1, 1, 4, true);
+  return check_ranges(ranges.r, ranges.n);
+}
+
+int check_clip(const dion_grad* list, int count, float max_norm, int norm_type, const float* norms, int num_norms,
+               const float* norm_out, const float* coef_out) {
+  if (count < 0 || (count > 0 && list == nullptr) || !norm_type_ok(norm_type) || !(max_norm >= 0.f)) return DION_ERR_INVALID;
+  if ((norms == nullptr) != (num_norms == 0) || num_norms < 0) return DION_ERR_INVALID;
+  LIST_TRY(check_floats(norms));
+  LIST_TRY(check_floats(norm_out));
+  LIST_TRY(check_floats(coef_out));
+  Ranges ranges(2 * (size_t)count + 3);
+  if (ranges.r == nullptr) return DION_ERR_NOMEM;
+  for (int i = 0; i < count; ++i) {
+    const dion_grad& a = list[i];
+    if (!known_type(a.g_dtype) || !known_type(a.out_dtype)) return DION_ERR_INVALID;
+    LIST_TRY(check_shape(a.rows, a.cols));
+    LIST_TRY(check_array(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype)));
+    LIST_TRY(check_array(a.out, a.rows, a.cols, a.ldo, bytes_of(a.out_dtype)));
+    const bool in_place = a.G == a.out && a.g_dtype == a.out_dtype && (a.ldg == a.ldo || a.rows <= 1);
+    ranges.add(a.out, a.rows, a.cols, a.ldo, bytes_of(a.out_dtype), true);
+    if (!in_place) ranges.add(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype), false);
+  }
+  ranges.add(norms, 1, num_norms, num_norms, 4, false);
+  ranges.add(norm_out, 1, 1, 1, 4, true);
+  ranges.add(coef_out, 1, 1, 1, 4, true);
+  return check_ranges(ranges.r, ranges.n);
+}
+
+int check_step(bool adamw, const dion_param* list, int count, const dion_rule* rule, float lr) {
+  if (count < 0 || (count > 0 && list == nullptr) || rule == nullptr || !isfinite(lr)) return DION_ERR_INVALID;
+  if (!(rule->beta1 >= 0.0 && rule->beta1 < 1.0) || !(rule->beta2 >= 0.0 && rule->beta2 < 1.0)) return DION_ERR_INVALID;
+  if (adamw && (!(rule->eps >= 0.0) || !isfinite(rule->eps) || (rule->step_dev == nullptr && rule->step < 1))) return DION_ERR_INVALID;
+  if ((uintptr_t)rule->step_dev & 7) return DION_ERR_ALIGN;
+  LIST_TRY(check_floats(rule->grad_scale));
+  Ranges ranges(5 * (size_t)count + 2);
+  if (ranges.r == nullptr) return DION_ERR_NOMEM;
+  // (kind by kind: the arrays of one kind are often views of one buffer, in its order)
+  for (int i = 0; i < count; ++i) {
+    const dion_param& a = list[i];
+    if (!known_type(a.g_dtype) || !known_type(a.m_dtype) || !isfinite(a.lr_scale) || !isfinite(a.weight_decay)) return DION_ERR_INVALID;
+    LIST_TRY(check_shape(a.rows, a.cols));
+    LIST_TRY(check_array(a.X, a.rows, a.cols, a.ldx, 4));
+    LIST_TRY(check_array(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype)));
+    LIST_TRY(check_array(a.M, a.rows, a.cols, a.ldm, bytes_of(a.m_dtype)));
+    if (adamw) LIST_TRY(check_array(a.V, a.rows, a.cols, a.ldv, 4));
+    if (a.X16 != nullptr) LIST_TRY(check_array(a.X16, a.rows, a.cols, a.ldx16, 2));
+    ranges.add(a.X, a.rows, a.cols, a.ldx, 4, true);
+  }
+  for (int i = 0; i < count; ++i) ranges.add(list[i].G, list[i].rows, list[i].cols, list[i].ldg, bytes_of(list[i].g_dtype), false);
+  for (int i = 0; i < count; ++i) ranges.add(list[i].M, list[i].rows, list[i].cols, list[i].ldm, bytes_of(list[i].m_dtype), true);
+  for (int i = 0; i < count && adamw; ++i) ranges.add(list[i].V, list[i].rows, list[i].cols, list[i].ldv, 4, true);
+  for (int i = 0; i < count; ++i) ranges.add(list[i].X16, list[i].rows, list[i].cols, list[i].ldx16, 2, true);
+  if (adamw) ranges.add(rule->step_dev, 1, 1, 1, 8, false);
+  ranges.add(rule->grad_scale, 1, 1, 1, 4, false);
+  return check_ranges(ranges.r, ranges.n);
+}
+
+int grad_norm(const Where& w, const dion_grad* list, int count, int norm_type, float max_norm, float* norm_out, float* each_out,
+              float* coef_out) {
+  NormOut o = {};
+  o.scratch = (Scratch*)w.scratch;
+  o.norm = norm_out; o.coef = coef_out; o.max_norm = max_norm;
+  o.status = w.status;
+  const bool inf = norm_type == DION_NORM_INF;
+  return count <= FEW ? norm_launches<FEW>(w, list, count, inf, o, each_out) : norm_launches<MANY_NORM>(w, list, count, inf, o, each_out);
+}
+
+int clip_grads(const Where& w, const dion_grad* list, int count, float max_norm, int norm_type, const float* norms, int num_norms,
+               float* norm_out, float* coef_out) {
+  Clip c = {};
+  c.max_norm = max_norm; c.inf = norm_type == DION_NORM_INF;
+  c.status = w.status;
+  if (norms != nullptr) {
+    c.norms = norms; c.count = num_norms; c.norm_out = norm_out; c.coef_out = coef_out;
+  } else {
+    LIST_TRY(grad_norm(w, list, count, norm_type, max_norm, norm_out, nullptr, coef_out));
+    if (count == 0) return DION_OK;
+    c.coef = &((Scratch*)w.scratch)->coef;
+  }
+  return count <= FEW ? scale_launches<FEW>(w, list, count, c) : scale_launches<MANY_SCALE>(w, list, count, c);
+}
+
+int param_step(const Where& w, bool adamw, const dion_param* list, int count, const dion_rule* rule, float lr) {
+  Rule r = {};
+  r.beta1 = rule->beta1; r.beta2 = rule->beta2;
+  r.b1 = (float)rule->beta1; r.c1 = (float)(1.0 - rule->beta1);
+  r.b2 = (float)rule->beta2; r.c2 = (float)(1.0 - rule->beta2);
+  r.eps = (float)rule->eps;
+  r.step_dev = adamw ? rule->step_dev : nullptr;
+  if (adamw && rule->step_dev == nullptr) {
+    r.inv1 = (float)(1.0 / (1.0 - pow(rule->beta1, (double)rule->step)));
+    r.inv2 = (float)(1.0 / (1.0 - pow(rule->beta2, (double)rule->step)));
+  }
+  r.scale = rule->grad_scale;
+  r.status = w.status;
+  if (adamw) return count <= FEW ? step_launches<FEW, true>(w, list, count, r, lr) : step_launches<MANY_STEP, true>(w, list, count, r, lr);
+  return count <= FEW ? step_launches<FEW, false>(w, list, count, r, lr) : step_launches<MANY_STEP, false>(w, list, count, r, lr);
+}
+
+}  // namespace list
+}  // namespace dion
