@@ -13,30 +13,42 @@ namespace dion {
 namespace list {
 
 constexpr int THREADS = 256;
-constexpr int TILE = 1024;       // elements of a tile
+constexpr int TILE_UNITS = 256;      // vectors of a tile, one per thread
+constexpr int TILE_SINGLES = 1024;   // elements of a tile that is walked one by one
+constexpr int W = 8;                 // elements of a vector: 32 bytes of fp32 (one load on sm_100), 16 of bf16
 
-// An array of n elements in rows of `cols` at a leading dimension (each pointer its own); dense arrays are one row.
-struct NormItem {
-  const void* g;
-  i64 n, cols, ldg;
+// How an array is walked.
+enum : int {
+  SINGLES = 0,       // element by element: the pointers' alignments differ, or rows are no whole vectors
+  DENSE = 1,         // one row: `head` elements up to the first 32-byte boundary, `units` vectors, the rest
+  SLICED = 2         // rows of `cols` vectors, all aligned
+};
+struct Walk {
+  i64 n, units, cols;            // elements; vectors (SINGLES: elements); of these in a row
   i64 first;                     // its first tile
+  int head, kind;
+};
+struct NormItem {
+  Walk w;
+  const void* g;
+  i64 ldg;
   int g_bf16;
 };
 struct ScaleItem {
+  Walk w;
   const void* g;
   void* out;
-  i64 n, cols, ldg, ldo;
-  i64 first;
+  i64 ldg, ldo;
   int g_bf16, o_bf16;
 };
 struct StepItem {
+  Walk w;
   float* X;
   const void* G;
   void* M;
   float* V;
   __nv_bfloat16* X16;
-  i64 n, cols, ldx, ldg, ldm, ldv, ldx16;
-  i64 first;
+  i64 ldx, ldg, ldm, ldv, ldx16;
   float lr, keep;                // lr * lr_scale; 1 - lr * lr_scale * weight_decay
   int g_bf16, m_bf16;
 };
@@ -92,7 +104,7 @@ __device__ __forceinline__ int find_item(const Table& t, i64 tile) {      // the
   int lo = 0, hi = t.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (t.item[mid].first <= tile) lo = mid; else hi = mid - 1;
+    if (t.item[mid].w.first <= tile) lo = mid; else hi = mid - 1;
   }
   return lo;
 }
@@ -105,16 +117,90 @@ __device__ __forceinline__ void store_as(void* p, i64 at, int bf16, float v) {
   else reinterpret_cast<float*>(p)[at] = v;
 }
 
-// Sums in 64 bits: squares of fp32 values neither overflow nor vanish there.  Maxima on the magnitudes' bits, whose order is
-// that of the values with NaN above infinity, so that a NaN is never lost.
+// Eight elements in one access: fp32 32 bytes, bf16 16.  Everything is touched once: not kept in L1.
+__device__ __forceinline__ void load_vec(const float* p, float (&x)[W]) {
+  asm volatile("ld.global.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(p));
+}
+__device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&x)[W]) {
+  uint32_t r[4];
+  asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+#pragma unroll
+  for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(r[k] << 16); x[2 * k + 1] = __uint_as_float(r[k] & 0xffff0000u); }
+}
+__device__ __forceinline__ void store_vec(float* p, const float (&x)[W]) {
+  asm volatile("st.global.L1::no_allocate.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               :: "l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
+}
+__device__ __forceinline__ void store_vec(__nv_bfloat16* p, const float (&x)[W]) {
+  uint32_t r[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+    r[k] = *reinterpret_cast<const uint32_t*>(&v);
+  }
+  asm volatile("st.global.L1::no_allocate.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+
+// A block's part of one array, in vectors (elements, if it is walked one by one); `ends`: with the elements before and behind
+// the vectors of a dense array.
+struct Part {
+  i64 u0, u1;
+  bool head, tail;
+};
+__device__ __forceinline__ Part part_of(const Walk& w, i64 tile, i64 end) {
+  const int per = w.kind == SINGLES ? TILE_SINGLES : TILE_UNITS;
+  Part p;
+  p.u0 = (tile - w.first) * per;
+  p.u1 = (end - w.first) * per;
+  p.tail = p.u1 >= w.units;
+  if (p.tail) p.u1 = w.units;
+  p.head = p.u0 == 0;
+  return p;
+}
+// The element at which vector u starts, in an array of this leading dimension; element e of one that is walked one by one.
+__device__ __forceinline__ i64 at_vector(const Walk& w, i64 u, i64 row, i64 ld) { return w.kind == DENSE ? w.head + u * W : row * ld + (u - row * w.cols) * W; }
+__device__ __forceinline__ i64 row_at(const Walk& w, i64 u) { return w.cols == w.units ? 0 : row_of(u, w.cols); }
+// Calls f(index) for the elements of a dense array that are in no vector.
+template <class F>
+__device__ __forceinline__ void ends_of(const Walk& w, const Part& p, F f) {
+  if (w.kind != DENSE) return;
+  if (p.head && (int)threadIdx.x < w.head) f((i64)threadIdx.x);
+  const i64 rest = w.head + w.units * W + threadIdx.x;
+  if (p.tail && rest < w.n) f(rest);
+}
+
+// Sums in 64 bits: squares of fp32 values neither overflow nor vanish there.  A group's squares are added in fp32 first (a
+// conversion and a 64-bit operation per element would cost more than the memory: 436M x 4 bf16 elements 6566 us); a sum that left
+// fp32's range, or came close enough to its lower end to have lost something, is taken again.  Maxima on the magnitudes'
+// bits, whose order is that of the values with NaN above infinity, so that a NaN is never lost.
 template <bool INF>
 struct Acc {
   double s = 0.0;
   uint32_t m = 0;
-  __device__ __forceinline__ void add(float x) {
-    if (INF) m = max(m, __float_as_uint(x) & 0x7fffffffu);
-    else s += (double)x * (double)x;
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N]) {
+    if (INF) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) m = max(m, __float_as_uint(x[k]) & 0x7fffffffu);
+      return;
+    }
+    float q = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) q = fmaf(x[k], x[k], q);
+    if (q >= 7.8886091e-31f && q <= 3.4028235e38f) {      // (2^-100: what is below 2^-149 in a square is nothing beside it)
+      s += (double)q;
+    } else {
+      bool any = false;
+#pragma unroll
+      for (int k = 0; k < N; ++k) any |= x[k] != 0.f;
+      if (any) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) s += (double)x[k] * (double)x[k];
+      }
+    }
   }
+  __device__ __forceinline__ void add(float x) { const float one[1] = {x}; add(one); }
   __device__ __forceinline__ void merge(double v) {        // a partial result as it is kept
     if (INF) m = max(m, __float_as_uint((float)v));
     else s += v;
@@ -145,6 +231,55 @@ __device__ __forceinline__ float clip_coef(float norm, float max_norm) {
   return !isfinite(norm) ? __int_as_float(0x7fffffff) : norm > max_norm ? max_norm / norm : 1.f;
 }
 
+template <bool INF, typename T>
+__device__ __forceinline__ void norm_vectors(const NormItem& it, const Part& p, Acc<INF>& acc) {
+  const T* g = reinterpret_cast<const T*>(it.g);
+  const Walk& w = it.w;
+  i64 u = p.u0 + threadIdx.x;
+  if (w.kind == DENSE) {
+    g += w.head;
+    for (; u + 3 * THREADS < p.u1; u += 4 * THREADS) {      // four loads in flight per thread
+      float x[4][W];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) load_vec(g + (u + k * THREADS) * W, x[k]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc.add(x[k]);
+    }
+    for (; u < p.u1; u += THREADS) {
+      float x[W];
+      load_vec(g + u * W, x);
+      acc.add(x);
+    }
+  } else {
+    for (; u < p.u1; u += THREADS) {
+      const i64 row = row_at(w, u);
+      float x[W];
+      load_vec(g + row * it.ldg + (u - row * w.cols) * W, x);
+      acc.add(x);
+    }
+  }
+}
+
+template <bool INF>
+__device__ __forceinline__ void norm_part(const NormItem& it, const Part& p, Acc<INF>& acc) {
+  if (it.w.kind == SINGLES) {
+    for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += 4 * THREADS) {
+      float x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const i64 f = e + k * THREADS, row = row_at(it.w, f);
+        x[k] = f < p.u1 ? load_as_float(it.g, row * it.ldg + (f - row * it.w.cols), it.g_bf16) : 0.f;
+      }
+      acc.add(x);
+    }
+  } else if (it.g_bf16) {
+    norm_vectors<INF, __nv_bfloat16>(it, p, acc);
+  } else {
+    norm_vectors<INF, float>(it, p, acc);
+  }
+  ends_of(it.w, p, [&](i64 e) { acc.add(load_as_float(it.g, e, it.g_bf16)); });
+}
+
 // Global norm: every block leaves its partial sums, the last one to finish adds them up in the order of the blocks.
 // With `each` a block leaves one sum per array that it touches, at [block + array]: both grow along the tiles, so no two share an
 // entry and those of one array are neighbours.
@@ -159,15 +294,10 @@ __global__ void __launch_bounds__(THREADS) k_list_norm(const __grid_constant__ T
   Acc<INF> acc;
   for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
     const NormItem& it = t.item[i];
-    i64 end = i + 1 < t.count ? t.item[i + 1].first : t.tiles;
+    i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
     if (end > t1) end = t1;
     if (end <= tile) continue;
-    i64 e1 = (end - it.first) * TILE;
-    if (e1 > it.n) e1 = it.n;
-    for (i64 e = (tile - it.first) * TILE + threadIdx.x; e < e1; e += THREADS) {
-      const i64 row = row_of(e, it.cols);
-      acc.add(load_as_float(it.g, row * it.ldg + (e - row * it.cols), it.g_bf16));
-    }
+    norm_part(it, part_of(it.w, tile, end), acc);
     if (each) {
       const Acc<INF> r = block_reduce(acc, red);
       if (threadIdx.x == 0) s->part[blockIdx.x + i] = r.kept();
@@ -188,7 +318,7 @@ __global__ void __launch_bounds__(THREADS) k_list_norm(const __grid_constant__ T
   if (each) {
     // a warp per array: its first and last block are those that own its first and last tile
     for (int i = threadIdx.x >> 5; i < t.count; i += THREADS / 32) {
-      const i64 f = t.item[i].first, l = (i + 1 < t.count ? t.item[i + 1].first : t.tiles) - 1;
+      const i64 f = t.item[i].w.first, l = (i + 1 < t.count ? t.item[i + 1].w.first : t.tiles) - 1;
       Acc<INF> a;
       if (f <= l) {
         const i64 b0 = ((f + 1) * G - 1) / t.tiles, b1 = ((l + 1) * G - 1) / t.tiles;
@@ -215,6 +345,21 @@ __global__ void __launch_bounds__(THREADS) k_list_norm(const __grid_constant__ T
   s->coef = coef;
   if (o.norm != nullptr) *o.norm = norm;
   if (o.coef != nullptr) *o.coef = coef;
+}
+
+template <typename TG, typename TO>
+__device__ __forceinline__ void scale_vectors(const ScaleItem& it, const Part& p, float coef) {
+  const TG* g = reinterpret_cast<const TG*>(it.g);
+  TO* out = reinterpret_cast<TO*>(it.out);
+  for (i64 u = p.u0 + (p.u1 - p.u0 - 1) / THREADS * THREADS + threadIdx.x; u >= p.u0; u -= THREADS) {
+    if (u >= p.u1) continue;
+    const i64 row = row_at(it.w, u);
+    float x[W];
+    load_vec(g + at_vector(it.w, u, row, it.ldg), x);
+#pragma unroll
+    for (int k = 0; k < W; ++k) x[k] *= coef;
+    store_vec(out + at_vector(it.w, u, row, it.ldo), x);
+  }
 }
 
 // out = coefficient * G.  Where G itself would be multiplied by one nothing is read or written.
@@ -247,19 +392,26 @@ __global__ void __launch_bounds__(THREADS) k_list_scale(const __grid_constant__ 
     coef = shared_coef;
   }
   const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
-  for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
+  // from the back: what the norm's launch read last is still in L2
+  for (i64 end = t1, i = t0 < t1 ? find_item(t, t1 - 1) : 0; end > t0; --i) {
     const ScaleItem& it = t.item[i];
-    i64 end = i + 1 < t.count ? t.item[i + 1].first : t.tiles;
-    if (end > t1) end = t1;
-    if (end <= tile) continue;
-    i64 e1 = (end - it.first) * TILE;
-    if (e1 > it.n) e1 = it.n;
-    if (!(coef == 1.f && it.g == it.out))
-      for (i64 e = (tile - it.first) * TILE + threadIdx.x; e < e1; e += THREADS) {
-        const i64 row = row_of(e, it.cols), col = e - row * it.cols;
-        store_as(it.out, row * it.ldo + col, it.o_bf16, coef * load_as_float(it.g, row * it.ldg + col, it.g_bf16));
+    const i64 tile = it.w.first > t0 ? it.w.first : t0;
+    if (tile >= end) continue;
+    if (!(coef == 1.f && it.g == it.out)) {
+      const Part p = part_of(it.w, tile, end);
+      if (it.w.kind == SINGLES) {
+        for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += THREADS) {
+          const i64 row = row_at(it.w, e), col = e - row * it.w.cols;
+          store_as(it.out, row * it.ldo + col, it.o_bf16, coef * load_as_float(it.g, row * it.ldg + col, it.g_bf16));
+        }
+      } else if (it.g_bf16) {
+        if (it.o_bf16) scale_vectors<__nv_bfloat16, __nv_bfloat16>(it, p, coef); else scale_vectors<__nv_bfloat16, float>(it, p, coef);
+      } else {
+        if (it.o_bf16) scale_vectors<float, __nv_bfloat16>(it, p, coef); else scale_vectors<float, float>(it, p, coef);
       }
-    tile = end;
+      ends_of(it.w, p, [&](i64 e) { store_as(it.out, e, it.o_bf16, coef * load_as_float(it.g, e, it.g_bf16)); });
+    }
+    end = tile;
   }
 }
 
@@ -285,6 +437,42 @@ __device__ __forceinline__ void step_element(const Rule& r, float inv1, float in
   } else {
     x = fmaf(-lr, lion_sign(r, m, g, s), x * keep);
     m = fmaf(r.b2, m, r.c2 * (s * g));
+  }
+}
+
+template <bool ADAMW>
+__device__ __forceinline__ void step_single(const StepItem& it, const Rule& r, float inv1, float inv2, float s, i64 row, i64 col) {
+  const float g = load_as_float(it.G, row * it.ldg + col, it.g_bf16);
+  float x = it.X[row * it.ldx + col], m = load_as_float(it.M, row * it.ldm + col, it.m_bf16), v = 0.f;
+  if (ADAMW) v = it.V[row * it.ldv + col];
+  step_element<ADAMW>(r, inv1, inv2, s, it.lr, it.keep, x, m, v, g);
+  it.X[row * it.ldx + col] = x;
+  store_as(it.M, row * it.ldm + col, it.m_bf16, m);
+  if (ADAMW) it.V[row * it.ldv + col] = v;
+  if (it.X16 != nullptr) it.X16[row * it.ldx16 + col] = __float2bfloat16_rn(x);
+}
+
+template <bool ADAMW, typename TG, typename TM>
+__device__ __forceinline__ void step_vectors(const StepItem& it, const Part& p, const Rule& r, float inv1, float inv2, float s) {
+  for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) {
+    const i64 row = row_at(it.w, u);
+    float* px = it.X + at_vector(it.w, u, row, it.ldx);
+    TM* pm = reinterpret_cast<TM*>(it.M) + at_vector(it.w, u, row, it.ldm);
+    float* pv = ADAMW ? it.V + at_vector(it.w, u, row, it.ldv) : nullptr;
+    float x[W], m[W], v[W], g[W];
+    load_vec(reinterpret_cast<const TG*>(it.G) + at_vector(it.w, u, row, it.ldg), g);
+    load_vec(pm, m);
+    if (ADAMW) load_vec(pv, v);
+    load_vec(px, x);
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      float none = 0.f;
+      step_element<ADAMW>(r, inv1, inv2, s, it.lr, it.keep, x[k], m[k], ADAMW ? v[k] : none, g[k]);
+    }
+    store_vec(px, x);
+    store_vec(pm, m);
+    if (ADAMW) store_vec(pv, v);
+    if (it.X16 != nullptr) store_vec(it.X16 + at_vector(it.w, u, row, it.ldx16), x);
   }
 }
 
@@ -318,22 +506,23 @@ __global__ void __launch_bounds__(THREADS) k_list_step(const __grid_constant__ T
   const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
   for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
     const StepItem& it = t.item[i];
-    i64 end = i + 1 < t.count ? t.item[i + 1].first : t.tiles;
+    i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
     if (end > t1) end = t1;
     if (end <= tile) continue;
-    i64 e1 = (end - it.first) * TILE;
-    if (e1 > it.n) e1 = it.n;
-    for (i64 e = (tile - it.first) * TILE + threadIdx.x; e < e1; e += THREADS) {
-      const i64 row = row_of(e, it.cols), col = e - row * it.cols;
-      const float g = load_as_float(it.G, row * it.ldg + col, it.g_bf16);
-      float x = it.X[row * it.ldx + col], m = load_as_float(it.M, row * it.ldm + col, it.m_bf16), v = 0.f;
-      if (ADAMW) v = it.V[row * it.ldv + col];
-      step_element<ADAMW>(r, inv1, inv2, s, it.lr, it.keep, x, m, v, g);
-      it.X[row * it.ldx + col] = x;
-      store_as(it.M, row * it.ldm + col, it.m_bf16, m);
-      if (ADAMW) it.V[row * it.ldv + col] = v;
-      if (it.X16 != nullptr) it.X16[row * it.ldx16 + col] = __float2bfloat16_rn(x);
+    const Part p = part_of(it.w, tile, end);
+    if (it.w.kind == SINGLES) {
+      for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += THREADS) {
+        const i64 row = row_at(it.w, e);
+        step_single<ADAMW>(it, r, inv1, inv2, s, row, e - row * it.w.cols);
+      }
+    } else if (it.g_bf16) {
+      if (it.m_bf16) step_vectors<ADAMW, __nv_bfloat16, __nv_bfloat16>(it, p, r, inv1, inv2, s);
+      else step_vectors<ADAMW, __nv_bfloat16, float>(it, p, r, inv1, inv2, s);
+    } else {
+      if (it.m_bf16) step_vectors<ADAMW, float, __nv_bfloat16>(it, p, r, inv1, inv2, s);
+      else step_vectors<ADAMW, float, float>(it, p, r, inv1, inv2, s);
     }
+    ends_of(it.w, p, [&](i64 e) { step_single<ADAMW>(it, r, inv1, inv2, s, 0, e); });
     tile = end;
   }
 }

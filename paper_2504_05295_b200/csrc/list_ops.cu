@@ -16,7 +16,7 @@ namespace {
 constexpr int BLOCKS_PER_SM = 8;
 // Arrays in one launch: its parameters end at 32764 bytes.  Small lists take small parameters.
 constexpr int FEW = 24;
-constexpr int MANY_NORM = 500, MANY_SCALE = 400, MANY_STEP = 250;
+constexpr int MANY_NORM = 500, MANY_SCALE = 400, MANY_STEP = 236;
 constexpr i64 MAX_ELEMENTS = (i64)1 << 50;      // (no element count or byte offset overflows)
 
 template <typename... KArgs, typename... Args>
@@ -109,18 +109,48 @@ int check_floats(const float* p) { return (uintptr_t)p & 3 ? DION_ERR_ALIGN : DI
     if (rc_ != DION_OK) return rc_; \
   } while (0)
 
-// Dense arrays are one row.
-void flatten(i64 rows, i64 cols, bool dense, i64* n, i64* row) {
-  *n = rows * cols;
-  *row = dense || rows == 1 ? *n : cols;
-  if (*row < 1) *row = 1;
-}
+// An array (of those that are walked together) as the walk needs it.
+struct Array {
+  const void* p;
+  i64 ld;
+  int size;
+};
 
-template <class Item, int CAP>
-i64 add_tiles(Table<Item, CAP>* t, Item* it) {
-  it->first = t->tiles;
-  t->tiles += (it->n + TILE - 1) / TILE;
-  return t->tiles;
+// How arrays of rows x cols are walked together, and their tiles behind the `tiles` so far.
+template <size_t N>
+Walk plan(i64 rows, i64 cols, const Array (&a)[N], i64* tiles) {
+  Walk w = {};
+  w.n = rows * cols;
+  w.first = *tiles;
+  if (w.n == 0) return w;
+  // the elements by which the addresses are beyond whole vectors, if they agree
+  int phase = -1;
+  bool agree = true, dense = true, vectors = cols % W == 0;
+  for (const Array& x : a) {
+    if (x.p == nullptr) continue;
+    const int ph = (int)((uintptr_t)x.p / x.size % W);
+    agree = agree && (phase < 0 || ph == phase);
+    phase = ph;
+    dense = dense && (rows == 1 || x.ld == cols);
+    vectors = vectors && ph == 0 && x.ld % W == 0;
+  }
+  if (dense && agree) {
+    w.kind = DENSE;
+    w.head = (int)std::min<i64>((W - phase) % W, w.n);
+    w.units = (w.n - w.head) / W;
+    w.cols = w.units;
+  } else if (vectors) {
+    w.kind = SLICED;
+    w.units = w.n / W;
+    w.cols = cols / W;
+  } else {
+    w.kind = SINGLES;
+    w.units = w.n;
+    w.cols = dense ? w.n : cols;
+  }
+  const i64 per = w.kind == SINGLES ? TILE_SINGLES : TILE_UNITS;
+  *tiles += std::max<i64>((w.units + per - 1) / per, 1);
+  return w;
 }
 
 template <int CAP>
@@ -134,8 +164,8 @@ int norm_launches(const Where& w, const dion_grad* list, int count, bool inf, No
       const dion_grad& a = list[done + i];
       NormItem* it = &t.item[i];
       it->g = a.G; it->g_bf16 = a.g_dtype == DION_BF16; it->ldg = a.ldg;
-      flatten(a.rows, a.cols, a.ldg == a.cols, &it->n, &it->cols);
-      add_tiles(&t, it);
+      const Array arrays[] = {{a.G, a.ldg, bytes_of(a.g_dtype)}};
+      it->w = plan(a.rows, a.cols, arrays, &t.tiles);
     }
     o.each = each != nullptr ? each + done : nullptr;
     o.use_carry = done > 0;
@@ -159,8 +189,8 @@ int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
       ScaleItem* it = &t.item[i];
       it->g = a.G; it->g_bf16 = a.g_dtype == DION_BF16; it->ldg = a.ldg;
       it->out = a.out; it->o_bf16 = a.out_dtype == DION_BF16; it->ldo = a.ldo;
-      flatten(a.rows, a.cols, a.ldg == a.cols && a.ldo == a.cols, &it->n, &it->cols);
-      add_tiles(&t, it);
+      const Array arrays[] = {{a.G, a.ldg, bytes_of(a.g_dtype)}, {a.out, a.ldo, bytes_of(a.out_dtype)}};
+      it->w = plan(a.rows, a.cols, arrays, &t.tiles);
     }
     done += t.count;
     LIST_TRY(launch(w, k_list_scale<CAP>, t.tiles, t, c));
@@ -186,9 +216,8 @@ int step_launches(const Where& w, const dion_param* list, int count, Rule r, flo
       it->X16 = (__nv_bfloat16*)a.X16; it->ldx16 = a.ldx16;
       it->lr = lr * a.lr_scale;
       it->keep = (float)(1.0 - (double)lr * a.lr_scale * a.weight_decay);
-      flatten(a.rows, a.cols, a.ldx == a.cols && a.ldg == a.cols && a.ldm == a.cols && (!ADAMW || a.ldv == a.cols) &&
-                              (a.X16 == nullptr || a.ldx16 == a.cols), &it->n, &it->cols);
-      add_tiles(&t, it);
+      const Array arrays[] = {{it->X, a.ldx, 4}, {a.G, a.ldg, bytes_of(a.g_dtype)}, {a.M, a.ldm, bytes_of(a.m_dtype)}, {it->V, a.ldv, 4}, {it->X16, a.ldx16, 2}};
+      it->w = plan(a.rows, a.cols, arrays, &t.tiles);
     }
     r.first = done == 0;
     done += t.count;
