@@ -13,6 +13,7 @@ namespace dion {
 namespace list {
 
 constexpr int THREADS = 256;
+constexpr int NORM_RESIDENT = 4, SCALE_RESIDENT = 4, ADAMW_RESIDENT = 3, LION_RESIDENT = 4;      // blocks per SM
 constexpr int TILE_UNITS = 256;      // vectors of a tile, one per thread
 constexpr int TILE_SINGLES = 1024;   // elements of a tile that is walked one by one
 constexpr int W = 8;                 // elements of a vector: 32 bytes of fp32 (one load on sm_100), 16 of bf16
@@ -158,8 +159,7 @@ __device__ __forceinline__ Part part_of(const Walk& w, i64 tile, i64 end) {
   p.head = p.u0 == 0;
   return p;
 }
-// The element at which vector u starts, in an array of this leading dimension; element e of one that is walked one by one.
-__device__ __forceinline__ i64 at_vector(const Walk& w, i64 u, i64 row, i64 ld) { return w.kind == DENSE ? w.head + u * W : row * ld + (u - row * w.cols) * W; }
+// The row of vector u (of element u in an array that is walked one by one).
 __device__ __forceinline__ i64 row_at(const Walk& w, i64 u) { return w.cols == w.units ? 0 : row_of(u, w.cols); }
 // Calls f(index) for the elements of a dense array that are in no vector.
 template <class F>
@@ -284,7 +284,7 @@ __device__ __forceinline__ void norm_part(const NormItem& it, const Part& p, Acc
 // With `each` a block leaves one sum per array that it touches, at [block + array]: both grow along the tiles, so no two share an
 // entry and those of one array are neighbours.
 template <int CAP, bool INF>
-__global__ void __launch_bounds__(THREADS) k_list_norm(const __grid_constant__ Table<NormItem, CAP> t, const NormOut o) {
+__global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __grid_constant__ Table<NormItem, CAP> t, const NormOut o) {
   __shared__ double red[THREADS / 32];
   __shared__ bool last;
   pdl_enter();
@@ -347,24 +347,40 @@ __global__ void __launch_bounds__(THREADS) k_list_norm(const __grid_constant__ T
   if (o.coef != nullptr) *o.coef = coef;
 }
 
+template <typename TG, typename TO, int N>
+__device__ __forceinline__ void scale_some(const TG* g, TO* out, float coef) {      // N vectors, THREADS apart
+  float x[N][W];
+#pragma unroll
+  for (int k = 0; k < N; ++k) load_vec(g + k * THREADS * W, x[k]);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+#pragma unroll
+    for (int q = 0; q < W; ++q) x[k][q] *= coef;
+    store_vec(out + k * THREADS * W, x[k]);
+  }
+}
+
 template <typename TG, typename TO>
 __device__ __forceinline__ void scale_vectors(const ScaleItem& it, const Part& p, float coef) {
   const TG* g = reinterpret_cast<const TG*>(it.g);
   TO* out = reinterpret_cast<TO*>(it.out);
-  for (i64 u = p.u0 + (p.u1 - p.u0 - 1) / THREADS * THREADS + threadIdx.x; u >= p.u0; u -= THREADS) {
-    if (u >= p.u1) continue;
-    const i64 row = row_at(it.w, u);
-    float x[W];
-    load_vec(g + at_vector(it.w, u, row, it.ldg), x);
-#pragma unroll
-    for (int k = 0; k < W; ++k) x[k] *= coef;
-    store_vec(out + at_vector(it.w, u, row, it.ldo), x);
+  i64 u = p.u0 + threadIdx.x;
+  if (it.w.kind == DENSE) {
+    g += it.w.head;
+    out += it.w.head;
+    for (; u + 3 * THREADS < p.u1; u += 4 * THREADS) scale_some<TG, TO, 4>(g + u * W, out + u * W, coef);
+    for (; u < p.u1; u += THREADS) scale_some<TG, TO, 1>(g + u * W, out + u * W, coef);
+  } else {
+    for (; u < p.u1; u += THREADS) {
+      const i64 row = row_at(it.w, u), col = (u - row * it.w.cols) * W;
+      scale_some<TG, TO, 1>(g + row * it.ldg + col, out + row * it.ldo + col, coef);
+    }
   }
 }
 
 // out = coefficient * G.  Where G itself would be multiplied by one nothing is read or written.
 template <int CAP>
-__global__ void __launch_bounds__(THREADS) k_list_scale(const __grid_constant__ Table<ScaleItem, CAP> t, const Clip c) {
+__global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __grid_constant__ Table<ScaleItem, CAP> t, const Clip c) {
   __shared__ double red[THREADS / 32];
   __shared__ float shared_coef;
   pdl_enter();
@@ -391,12 +407,13 @@ __global__ void __launch_bounds__(THREADS) k_list_scale(const __grid_constant__ 
     __syncthreads();
     coef = shared_coef;
   }
-  const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
-  // from the back: what the norm's launch read last is still in L2
-  for (i64 end = t1, i = t0 < t1 ? find_item(t, t1 - 1) : 0; end > t0; --i) {
+  // the last blocks of the list first: what the norm's launch read last is still in L2
+  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = t.tiles * b / G, t1 = t.tiles * (b + 1) / G;
+  for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
     const ScaleItem& it = t.item[i];
-    const i64 tile = it.w.first > t0 ? it.w.first : t0;
-    if (tile >= end) continue;
+    i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
+    if (end > t1) end = t1;
+    if (end <= tile) continue;
     if (!(coef == 1.f && it.g == it.out)) {
       const Part p = part_of(it.w, tile, end);
       if (it.w.kind == SINGLES) {
@@ -411,7 +428,7 @@ __global__ void __launch_bounds__(THREADS) k_list_scale(const __grid_constant__ 
       }
       ends_of(it.w, p, [&](i64 e) { store_as(it.out, e, it.o_bf16, coef * load_as_float(it.g, e, it.g_bf16)); });
     }
-    end = tile;
+    tile = end;
   }
 }
 
@@ -453,31 +470,42 @@ __device__ __forceinline__ void step_single(const StepItem& it, const Rule& r, f
 }
 
 template <bool ADAMW, typename TG, typename TM>
-__device__ __forceinline__ void step_vectors(const StepItem& it, const Part& p, const Rule& r, float inv1, float inv2, float s) {
-  for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) {
-    const i64 row = row_at(it.w, u);
-    float* px = it.X + at_vector(it.w, u, row, it.ldx);
-    TM* pm = reinterpret_cast<TM*>(it.M) + at_vector(it.w, u, row, it.ldm);
-    float* pv = ADAMW ? it.V + at_vector(it.w, u, row, it.ldv) : nullptr;
-    float x[W], m[W], v[W], g[W];
-    load_vec(reinterpret_cast<const TG*>(it.G) + at_vector(it.w, u, row, it.ldg), g);
-    load_vec(pm, m);
-    if (ADAMW) load_vec(pv, v);
-    load_vec(px, x);
+__device__ __forceinline__ void step_vector(const StepItem& it, const Rule& r, float inv1, float inv2, float s, float* px, const TG* pg, TM* pm, float* pv, __nv_bfloat16* p16) {
+  float x[W], m[W], v[W], g[W];
+  load_vec(pg, g);
+  load_vec(pm, m);
+  if (ADAMW) load_vec(pv, v);
+  load_vec(px, x);
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      float none = 0.f;
-      step_element<ADAMW>(r, inv1, inv2, s, it.lr, it.keep, x[k], m[k], ADAMW ? v[k] : none, g[k]);
+  for (int k = 0; k < W; ++k) {
+    float none = 0.f;
+    step_element<ADAMW>(r, inv1, inv2, s, it.lr, it.keep, x[k], m[k], ADAMW ? v[k] : none, g[k]);
+  }
+  store_vec(px, x);
+  store_vec(pm, m);
+  if (ADAMW) store_vec(pv, v);
+  if (it.X16 != nullptr) store_vec(p16, x);
+}
+
+template <bool ADAMW, typename TG, typename TM>
+__device__ __forceinline__ void step_vectors(const StepItem& it, const Part& p, const Rule& r, float inv1, float inv2, float s) {
+  const TG* G = reinterpret_cast<const TG*>(it.G);
+  TM* M = reinterpret_cast<TM*>(it.M);
+  if (it.w.kind == DENSE) {
+    for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) {
+      const i64 e = it.w.head + u * W;
+      step_vector<ADAMW>(it, r, inv1, inv2, s, it.X + e, G + e, M + e, it.V + e, it.X16 + e);
     }
-    store_vec(px, x);
-    store_vec(pm, m);
-    if (ADAMW) store_vec(pv, v);
-    if (it.X16 != nullptr) store_vec(it.X16 + at_vector(it.w, u, row, it.ldx16), x);
+  } else {
+    for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) {
+      const i64 row = row_at(it.w, u), col = (u - row * it.w.cols) * W;
+      step_vector<ADAMW>(it, r, inv1, inv2, s, it.X + row * it.ldx + col, G + row * it.ldg + col, M + row * it.ldm + col, it.V + row * it.ldv + col, it.X16 + row * it.ldx16 + col);
+    }
   }
 }
 
 template <int CAP, bool ADAMW>
-__global__ void __launch_bounds__(THREADS) k_list_step(const __grid_constant__ Table<StepItem, CAP> t, const Rule r) {
+__global__ void __launch_bounds__(THREADS, ADAMW ? ADAMW_RESIDENT : LION_RESIDENT) k_list_step(const __grid_constant__ Table<StepItem, CAP> t, const Rule r) {
   __shared__ float corr[2];
   pdl_enter();
   const float s = r.scale != nullptr ? *r.scale : 1.f;

@@ -149,7 +149,7 @@ def test_binding_refuses_host_tensors():
     with pytest.raises(ValueError, match="CUDA"):
         binding.grad_list([t])
     with pytest.raises(ValueError, match="CUDA"):
-        binding.param_desc(t, t, t)
+        binding.param_list([binding.param_desc(t, t, t)])
     with pytest.raises(ValueError, match="as many"):
         binding.grad_list([t], [])
 
