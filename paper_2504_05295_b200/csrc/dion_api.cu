@@ -2587,7 +2587,7 @@ int dion_init(dion_ctx** out, const dion_config* cfg) {
   c->sm_count = prop.multiProcessorCount;
   void* p = nullptr;
   constexpr size_t ctl_bytes = (sizeof(int) * (8 + MAX_FLAG_SLOTS * OS_SLOT_INTS + 24 + FLOW_CTL_INTS) + 127) / 128 * 128;
-  const size_t int_bytes = ctl_bytes + list::scratch_bytes(c->sm_count);
+  const size_t int_bytes = ctl_bytes + list::scratch_bytes();
   if (cudaMalloc(&p, int_bytes) != cudaSuccess) { delete c; return DION_ERR_NOMEM; }
   c->dev_ints = (int*)p;
   c->flow_ctl = c->dev_ints + 8 + MAX_FLAG_SLOTS * OS_SLOT_INTS + 24;      // (128-byte aligned)

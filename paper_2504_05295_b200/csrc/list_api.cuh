@@ -9,13 +9,13 @@ namespace list {
 // What a call needs of its context.
 struct Where {
   int sm_count;
-  void* scratch;          // scratch_bytes(sm_count), zero at first
+  void* scratch;          // scratch_bytes(), zero at first
   int* status;            // [0] status bits, [1] cancelled steps
   int64_t* launches;
   cudaStream_t stream;
 };
 
-size_t scratch_bytes(int sm_count);
+size_t scratch_bytes();
 
 // Loads every kernel (a kernel's first use could otherwise fall into a stream capture).
 int configure();

@@ -14,33 +14,34 @@ namespace list {
 
 constexpr int THREADS = 256;
 constexpr int NORM_RESIDENT = 4, SCALE_RESIDENT = 4, ADAMW_RESIDENT = 3, LION_RESIDENT = 4;      // blocks per SM
-constexpr int TILE_UNITS = 256;      // vectors of a tile, one per thread
-constexpr int TILE_SINGLES = 1024;   // elements of a tile that is walked one by one
-constexpr int W = 8;                 // elements of a vector: 32 bytes of fp32 (one load on sm_100), 16 of bf16
+constexpr int MOST_NORM_BLOCKS = 1024, MOST_PARTS = MOST_NORM_BLOCKS + 500;      // blocks of a norm launch; with its arrays
+constexpr int TILE_UNITS = 256;      // groups of a tile, one per thread
+constexpr int BATCH = 4;             // elements that a thread takes at once from an array that is walked one by one
+constexpr int W = 8;                 // elements of a group: 32 bytes of fp32 (one load on sm_100), 16 of bf16
 
-// How an array is walked.
-enum : int {
-  SINGLES = 0,       // element by element: the pointers' alignments differ, or rows are no whole vectors
-  DENSE = 1,         // one row: `head` elements up to the first 32-byte boundary, `units` vectors, the rest
-  SLICED = 2         // rows of `cols` vectors, all aligned
-};
+// How an array is walked.  Its rows are cut into groups of W elements at multiples of W elements of the ADDRESS, which is the same
+// cut for all arrays of an item: what lies wholly in its row is one access per array, what hangs over a row's end goes element
+// by element.  A row of `width` elements has groups at up to (width + 14) / 8 places, and each row is given that many.
+// One by one go items whose arrays' addresses (or leading dimensions) do not agree modulo W, and narrow rows, most of whose
+// groups would hang over an end.
 struct Walk {
-  i64 n, units, cols;            // elements; vectors (SINGLES: elements); of these in a row
   i64 first;                     // its first tile
-  int head, kind;
+  i64 units, per_row;            // groups, or elements; of these in a row
+  i64 width;                     // columns (of a dense array, which is one row: all elements)
+  uint8_t phase, shift;          // address of row 0 and leading dimension, in elements modulo W
+  bool singles;                  // one by one
+  bool g_bf16, other_bf16;       // types: of G; of the result or the moment
 };
 struct NormItem {
   Walk w;
   const void* g;
   i64 ldg;
-  int g_bf16;
 };
 struct ScaleItem {
   Walk w;
   const void* g;
   void* out;
   i64 ldg, ldo;
-  int g_bf16, o_bf16;
 };
 struct StepItem {
   Walk w;
@@ -51,7 +52,6 @@ struct StepItem {
   __nv_bfloat16* X16;
   i64 ldx, ldg, ldm, ldv, ldx16;
   float lr, keep;                // lr * lr_scale; 1 - lr * lr_scale * weight_decay
-  int g_bf16, m_bf16;
 };
 
 template <class Item, int CAP>
@@ -67,7 +67,7 @@ struct Scratch {
   float coef;                    // clipping coefficient for the launch behind
   double carry;                  // sum (or maximum) over the launches of a list that takes several
   double pad[14];
-  double part[1];                // one entry per block and array that it touches
+  double part[MOST_PARTS];       // one entry per block and array that it touches
 };
 
 struct NormOut {
@@ -100,15 +100,23 @@ struct Rule {
   int* status;                   // [0] bits, [1] cancelled steps
 };
 
+// The last array that starts at or before the tile.  Seven looks at a time: a look at the parameters is a round trip to memory
+// the first time, and these do not wait for one another.
 template <class Table>
-__device__ __forceinline__ int find_item(const Table& t, i64 tile) {      // the last array that starts at or before the tile
-  int lo = 0, hi = t.count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.item[mid].w.first <= tile) lo = mid; else hi = mid - 1;
+__device__ __forceinline__ int find_item(const Table& t, i64 tile) {
+  int lo = 0;
+  for (int span = t.count > 64 ? 64 : t.count > 8 ? 8 : 1; span > 0; span /= 8) {
+    int ahead = 0;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) {
+      const int at = lo + k * span;
+      if (at < t.count && t.item[at].w.first <= tile) ahead = k;
+    }
+    lo += ahead * span;
   }
   return lo;
 }
+static_assert(8 * 64 >= 500, "find_item reaches every array of a table");
 
 __device__ __forceinline__ float load_as_float(const void* p, i64 at, int bf16) {
   return bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[at]) : reinterpret_cast<const float*>(p)[at];
@@ -143,31 +151,56 @@ __device__ __forceinline__ void store_vec(__nv_bfloat16* p, const float (&x)[W])
   asm volatile("st.global.L1::no_allocate.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 
-// A block's part of one array, in vectors (elements, if it is walked one by one); `ends`: with the elements before and behind
-// the vectors of a dense array.
+// Elements lo to hi of a group, where p points to its (perhaps missing) element 0.
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_float(float* p, float x) { *p = x; }
+__device__ __forceinline__ void from_float(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+template <typename T>
+__device__ __forceinline__ void load_part(const T* p, float (&x)[W], int lo, int hi) {
+#pragma unroll
+  for (int k = 0; k < W; ++k) x[k] = k >= lo && k < hi ? to_float(p[k]) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T* p, const float (&x)[W], int lo, int hi) {
+#pragma unroll
+  for (int k = 0; k < W; ++k)
+    if (k >= lo && k < hi) from_float(p + k, x[k]);
+}
+template <typename T>
+__device__ __forceinline__ void load_group(const T* p, float (&x)[W], int lo, int hi) {
+  if (lo == 0 && hi == W) load_vec(p, x); else load_part(p, x, lo, hi);
+}
+template <typename T>
+__device__ __forceinline__ void store_group(T* p, const float (&x)[W], int lo, int hi) {
+  if (lo == 0 && hi == W) store_vec(p, x); else store_part(p, x, lo, hi);
+}
+
+// A block's part of one array, in groups or elements.
 struct Part {
   i64 u0, u1;
-  bool head, tail;
 };
 __device__ __forceinline__ Part part_of(const Walk& w, i64 tile, i64 end) {
-  const int per = w.kind == SINGLES ? TILE_SINGLES : TILE_UNITS;
+  const int per = w.singles ? THREADS * BATCH : TILE_UNITS;
   Part p;
   p.u0 = (tile - w.first) * per;
   p.u1 = (end - w.first) * per;
-  p.tail = p.u1 >= w.units;
-  if (p.tail) p.u1 = w.units;
-  p.head = p.u0 == 0;
+  if (p.u1 > w.units) p.u1 = w.units;
   return p;
 }
-// The row of vector u (of element u in an array that is walked one by one).
-__device__ __forceinline__ i64 row_at(const Walk& w, i64 u) { return w.cols == w.units ? 0 : row_of(u, w.cols); }
-// Calls f(index) for the elements of a dense array that are in no vector.
-template <class F>
-__device__ __forceinline__ void ends_of(const Walk& w, const Part& p, F f) {
-  if (w.kind != DENSE) return;
-  if (p.head && (int)threadIdx.x < w.head) f((i64)threadIdx.x);
-  const i64 rest = w.head + w.units * W + threadIdx.x;
-  if (p.tail && rest < w.n) f(rest);
+// Row and column of group u's element 0, and which of its elements exist; of element u in an array that is walked one by one.
+struct Spot {
+  i64 row, col;
+  int lo, hi;
+};
+__device__ __forceinline__ i64 row_at(const Walk& w, i64 u) { return w.per_row == w.units ? 0 : row_of(u, w.per_row); }
+__device__ __forceinline__ Spot group_at(const Walk& w, i64 u) {
+  Spot s;
+  s.row = row_at(w, u);
+  s.col = (u - s.row * w.per_row) * W - ((w.phase + (int)s.row * w.shift) & (W - 1));
+  s.lo = s.col < 0 ? (int)-s.col : 0;
+  s.hi = w.width - s.col < W ? (int)(w.width - s.col) : W;      // (below lo: a place that this row does not fill)
+  return s;
 }
 
 // Sums in 64 bits: squares of fp32 values neither overflow nor vanish there.  A group's squares are added in fp32 first (a
@@ -232,52 +265,56 @@ __device__ __forceinline__ float clip_coef(float norm, float max_norm) {
 }
 
 template <bool INF, typename T>
-__device__ __forceinline__ void norm_vectors(const NormItem& it, const Part& p, Acc<INF>& acc) {
+__device__ __forceinline__ void norm_groups(const NormItem& it, const Part& p, Acc<INF>& acc) {
   const T* g = reinterpret_cast<const T*>(it.g);
   const Walk& w = it.w;
   i64 u = p.u0 + threadIdx.x;
-  if (w.kind == DENSE) {
-    g += w.head;
-    for (; u + 3 * THREADS < p.u1; u += 4 * THREADS) {      // four loads in flight per thread
+  if (w.per_row == w.units) {
+    // one row: all but its first and last groups are whole, and four loads are in flight per thread
+    const i64 first = w.phase != 0, end = (w.width + w.phase) / W < p.u1 ? (w.width + w.phase) / W : p.u1;
+    const T* g0 = g - w.phase;
+    if (u < first) u += THREADS;
+    for (; u + 3 * THREADS < end; u += 4 * THREADS) {
       float x[4][W];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) load_vec(g + (u + k * THREADS) * W, x[k]);
+      for (int k = 0; k < 4; ++k) load_vec(g0 + (u + k * THREADS) * W, x[k]);
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc.add(x[k]);
     }
-    for (; u < p.u1; u += THREADS) {
+    for (; u < end; u += THREADS) {
       float x[W];
-      load_vec(g + u * W, x);
+      load_vec(g0 + u * W, x);
       acc.add(x);
     }
-  } else {
-    for (; u < p.u1; u += THREADS) {
-      const i64 row = row_at(w, u);
-      float x[W];
-      load_vec(g + row * it.ldg + (u - row * w.cols) * W, x);
-      acc.add(x);
-    }
+    // (thread 0 takes the first group, another one the last)
+    u = threadIdx.x == 0 && p.u0 < first ? 0 : threadIdx.x == 32 && end >= first && end < p.u1 ? end : p.u1;
+  }
+  for (; u < p.u1; u += THREADS) {
+    const Spot s = group_at(w, u);
+    float x[W];
+    load_group(g + s.row * it.ldg + s.col, x, s.lo, s.hi);
+    acc.add(x);
+    if (w.per_row == w.units) break;
   }
 }
 
 template <bool INF>
 __device__ __forceinline__ void norm_part(const NormItem& it, const Part& p, Acc<INF>& acc) {
-  if (it.w.kind == SINGLES) {
-    for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += 4 * THREADS) {
-      float x[4];
+  if (it.w.singles) {
+    for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += BATCH * THREADS) {
+      float x[BATCH];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < BATCH; ++k) {
         const i64 f = e + k * THREADS, row = row_at(it.w, f);
-        x[k] = f < p.u1 ? load_as_float(it.g, row * it.ldg + (f - row * it.w.cols), it.g_bf16) : 0.f;
+        x[k] = f < p.u1 ? load_as_float(it.g, row * it.ldg + (f - row * it.w.per_row), it.w.g_bf16) : 0.f;
       }
       acc.add(x);
     }
-  } else if (it.g_bf16) {
-    norm_vectors<INF, __nv_bfloat16>(it, p, acc);
+  } else if (it.w.g_bf16) {
+    norm_groups<INF, __nv_bfloat16>(it, p, acc);
   } else {
-    norm_vectors<INF, float>(it, p, acc);
+    norm_groups<INF, float>(it, p, acc);
   }
-  ends_of(it.w, p, [&](i64 e) { acc.add(load_as_float(it.g, e, it.g_bf16)); });
 }
 
 // Global norm: every block leaves its partial sums, the last one to finish adds them up in the order of the blocks.
@@ -287,12 +324,15 @@ template <int CAP, bool INF>
 __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __grid_constant__ Table<NormItem, CAP> t, const NormOut o) {
   __shared__ double red[THREADS / 32];
   __shared__ bool last;
-  pdl_enter();
+  __shared__ double parts[MOST_PARTS];
+  __shared__ i64 starts[CAP + 1];
   const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
+  i64 i = t0 < t1 ? find_item(t, t0) : 0;
+  pdl_enter();
   const bool each = o.each != nullptr;
   Scratch* s = o.scratch;
   Acc<INF> acc;
-  for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
+  for (i64 tile = t0; tile < t1; ++i) {
     const NormItem& it = t.item[i];
     i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
     if (end > t1) end = t1;
@@ -316,13 +356,17 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
   __threadfence();
   Acc<INF> all;
   if (each) {
-    // a warp per array: its first and last block are those that own its first and last tile
+    // every partial result in one round trip; then a warp per array, whose first and last block are those that own its
+    // first and last tile
+    for (int k = threadIdx.x; k < G + t.count; k += THREADS) parts[k] = __ldcg(&s->part[k]);
+    for (int i = threadIdx.x; i <= t.count; i += THREADS) starts[i] = i < t.count ? t.item[i].w.first : t.tiles;
+    __syncthreads();
     for (int i = threadIdx.x >> 5; i < t.count; i += THREADS / 32) {
-      const i64 f = t.item[i].w.first, l = (i + 1 < t.count ? t.item[i + 1].w.first : t.tiles) - 1;
+      const i64 f = starts[i], l = starts[i + 1] - 1;
       Acc<INF> a;
       if (f <= l) {
         const i64 b0 = ((f + 1) * G - 1) / t.tiles, b1 = ((l + 1) * G - 1) / t.tiles;
-        for (i64 b = b0 + (threadIdx.x & 31); b <= b1; b += 32) a.merge(__ldcg(&s->part[b + i]));
+        for (i64 b = b0 + (threadIdx.x & 31); b <= b1; b += 32) a.merge(parts[b + i]);
       }
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) {
@@ -361,19 +405,45 @@ __device__ __forceinline__ void scale_some(const TG* g, TO* out, float coef) {  
 }
 
 template <typename TG, typename TO>
-__device__ __forceinline__ void scale_vectors(const ScaleItem& it, const Part& p, float coef) {
+__device__ __forceinline__ void scale_groups(const ScaleItem& it, const Part& p, float coef) {
   const TG* g = reinterpret_cast<const TG*>(it.g);
   TO* out = reinterpret_cast<TO*>(it.out);
+  const Walk& w = it.w;
   i64 u = p.u0 + threadIdx.x;
-  if (it.w.kind == DENSE) {
-    g += it.w.head;
-    out += it.w.head;
-    for (; u + 3 * THREADS < p.u1; u += 4 * THREADS) scale_some<TG, TO, 4>(g + u * W, out + u * W, coef);
-    for (; u < p.u1; u += THREADS) scale_some<TG, TO, 1>(g + u * W, out + u * W, coef);
-  } else {
-    for (; u < p.u1; u += THREADS) {
-      const i64 row = row_at(it.w, u), col = (u - row * it.w.cols) * W;
-      scale_some<TG, TO, 1>(g + row * it.ldg + col, out + row * it.ldo + col, coef);
+  if (w.per_row == w.units) {      // one row: as in norm_groups
+    const i64 first = w.phase != 0, end = (w.width + w.phase) / W < p.u1 ? (w.width + w.phase) / W : p.u1;
+    const TG* g0 = g - w.phase;
+    TO* out0 = out - w.phase;
+    if (u < first) u += THREADS;
+    for (; u + 3 * THREADS < end; u += 4 * THREADS) scale_some<TG, TO, 4>(g0 + u * W, out0 + u * W, coef);
+    for (; u < end; u += THREADS) scale_some<TG, TO, 1>(g0 + u * W, out0 + u * W, coef);
+    u = threadIdx.x == 0 && p.u0 < first ? 0 : threadIdx.x == 32 && end >= first && end < p.u1 ? end : p.u1;
+  }
+  for (; u < p.u1; u += THREADS) {
+    const Spot s = group_at(w, u);
+    float x[W];
+    load_group(g + s.row * it.ldg + s.col, x, s.lo, s.hi);
+#pragma unroll
+    for (int k = 0; k < W; ++k) x[k] *= coef;
+    store_group(out + s.row * it.ldo + s.col, x, s.lo, s.hi);
+    if (w.per_row == w.units) break;
+  }
+}
+
+__device__ __forceinline__ void scale_singles(const ScaleItem& it, const Part& p, float coef) {
+  for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += BATCH * THREADS) {
+    float x[BATCH];
+    i64 row[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const i64 f = e + k * THREADS;
+      row[k] = row_at(it.w, f);
+      x[k] = f < p.u1 ? load_as_float(it.g, row[k] * it.ldg + (f - row[k] * it.w.per_row), it.w.g_bf16) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const i64 f = e + k * THREADS;
+      if (f < p.u1) store_as(it.out, row[k] * it.ldo + (f - row[k] * it.w.per_row), it.w.other_bf16, coef * x[k]);
     }
   }
 }
@@ -383,6 +453,9 @@ template <int CAP>
 __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __grid_constant__ Table<ScaleItem, CAP> t, const Clip c) {
   __shared__ double red[THREADS / 32];
   __shared__ float shared_coef;
+  // the last blocks of the list first: what the norm's launch read last is still in L2
+  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = t.tiles * b / G, t1 = t.tiles * (b + 1) / G;
+  i64 i = t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
   float coef;
   if (c.coef != nullptr) {
@@ -407,26 +480,20 @@ __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __
     __syncthreads();
     coef = shared_coef;
   }
-  // the last blocks of the list first: what the norm's launch read last is still in L2
-  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = t.tiles * b / G, t1 = t.tiles * (b + 1) / G;
-  for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
+  for (i64 tile = t0; tile < t1; ++i) {
     const ScaleItem& it = t.item[i];
     i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
     if (end > t1) end = t1;
     if (end <= tile) continue;
     if (!(coef == 1.f && it.g == it.out)) {
       const Part p = part_of(it.w, tile, end);
-      if (it.w.kind == SINGLES) {
-        for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += THREADS) {
-          const i64 row = row_at(it.w, e), col = e - row * it.w.cols;
-          store_as(it.out, row * it.ldo + col, it.o_bf16, coef * load_as_float(it.g, row * it.ldg + col, it.g_bf16));
-        }
-      } else if (it.g_bf16) {
-        if (it.o_bf16) scale_vectors<__nv_bfloat16, __nv_bfloat16>(it, p, coef); else scale_vectors<__nv_bfloat16, float>(it, p, coef);
+      if (it.w.singles) {
+        scale_singles(it, p, coef);
+      } else if (it.w.g_bf16) {
+        if (it.w.other_bf16) scale_groups<__nv_bfloat16, __nv_bfloat16>(it, p, coef); else scale_groups<__nv_bfloat16, float>(it, p, coef);
       } else {
-        if (it.o_bf16) scale_vectors<float, __nv_bfloat16>(it, p, coef); else scale_vectors<float, float>(it, p, coef);
+        if (it.w.other_bf16) scale_groups<float, __nv_bfloat16>(it, p, coef); else scale_groups<float, float>(it, p, coef);
       }
-      ends_of(it.w, p, [&](i64 e) { store_as(it.out, e, it.o_bf16, coef * load_as_float(it.g, e, it.g_bf16)); });
     }
     tile = end;
   }
@@ -458,55 +525,81 @@ __device__ __forceinline__ void step_element(const Rule& r, float inv1, float in
 }
 
 template <bool ADAMW>
-__device__ __forceinline__ void step_single(const StepItem& it, const Rule& r, float inv1, float inv2, float s, i64 row, i64 col) {
-  const float g = load_as_float(it.G, row * it.ldg + col, it.g_bf16);
-  float x = it.X[row * it.ldx + col], m = load_as_float(it.M, row * it.ldm + col, it.m_bf16), v = 0.f;
-  if (ADAMW) v = it.V[row * it.ldv + col];
-  step_element<ADAMW>(r, inv1, inv2, s, it.lr, it.keep, x, m, v, g);
-  it.X[row * it.ldx + col] = x;
-  store_as(it.M, row * it.ldm + col, it.m_bf16, m);
-  if (ADAMW) it.V[row * it.ldv + col] = v;
-  if (it.X16 != nullptr) it.X16[row * it.ldx16 + col] = __float2bfloat16_rn(x);
+__device__ __forceinline__ void step_singles(const StepItem& it, const Part& p, const Rule& r, float inv1, float inv2, float s) {
+  for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += BATCH * THREADS) {
+    float x[BATCH], m[BATCH], v[BATCH], g[BATCH];
+    i64 row[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {      // all loads first
+      i64 f = e + k * THREADS;
+      if (f >= p.u1) f = e;
+      row[k] = row_at(it.w, f);
+      const i64 col = f - row[k] * it.w.per_row;
+      g[k] = load_as_float(it.G, row[k] * it.ldg + col, it.w.g_bf16);
+      m[k] = load_as_float(it.M, row[k] * it.ldm + col, it.w.other_bf16);
+      v[k] = ADAMW ? it.V[row[k] * it.ldv + col] : 0.f;
+      x[k] = it.X[row[k] * it.ldx + col];
+    }
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const i64 f = e + k * THREADS, col = f - row[k] * it.w.per_row;
+      step_element<ADAMW>(r, inv1, inv2, s, it.lr, it.keep, x[k], m[k], v[k], g[k]);
+      if (f >= p.u1) continue;
+      it.X[row[k] * it.ldx + col] = x[k];
+      store_as(it.M, row[k] * it.ldm + col, it.w.other_bf16, m[k]);
+      if (ADAMW) it.V[row[k] * it.ldv + col] = v[k];
+      if (it.X16 != nullptr) it.X16[row[k] * it.ldx16 + col] = __float2bfloat16_rn(x[k]);
+    }
+  }
 }
 
 template <bool ADAMW, typename TG, typename TM>
-__device__ __forceinline__ void step_vector(const StepItem& it, const Rule& r, float inv1, float inv2, float s, float* px, const TG* pg, TM* pm, float* pv, __nv_bfloat16* p16) {
+__device__ __forceinline__ void step_group(const StepItem& it, const Rule& r, float inv1, float inv2, float s, float* px, const TG* pg, TM* pm, float* pv,
+                                           __nv_bfloat16* p16, int lo, int hi) {
   float x[W], m[W], v[W], g[W];
-  load_vec(pg, g);
-  load_vec(pm, m);
-  if (ADAMW) load_vec(pv, v);
-  load_vec(px, x);
+  load_group(pg, g, lo, hi);
+  load_group(pm, m, lo, hi);
+  if (ADAMW) load_group(pv, v, lo, hi);
+  load_group(px, x, lo, hi);
 #pragma unroll
   for (int k = 0; k < W; ++k) {
     float none = 0.f;
     step_element<ADAMW>(r, inv1, inv2, s, it.lr, it.keep, x[k], m[k], ADAMW ? v[k] : none, g[k]);
   }
-  store_vec(px, x);
-  store_vec(pm, m);
-  if (ADAMW) store_vec(pv, v);
-  if (it.X16 != nullptr) store_vec(p16, x);
+  store_group(px, x, lo, hi);
+  store_group(pm, m, lo, hi);
+  if (ADAMW) store_group(pv, v, lo, hi);
+  if (it.X16 != nullptr) store_group(p16, x, lo, hi);
 }
 
 template <bool ADAMW, typename TG, typename TM>
-__device__ __forceinline__ void step_vectors(const StepItem& it, const Part& p, const Rule& r, float inv1, float inv2, float s) {
+__device__ __forceinline__ void step_groups(const StepItem& it, const Part& p, const Rule& r, float inv1, float inv2, float s) {
   const TG* G = reinterpret_cast<const TG*>(it.G);
   TM* M = reinterpret_cast<TM*>(it.M);
-  if (it.w.kind == DENSE) {
-    for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) {
-      const i64 e = it.w.head + u * W;
-      step_vector<ADAMW>(it, r, inv1, inv2, s, it.X + e, G + e, M + e, it.V + e, it.X16 + e);
+  const Walk& w = it.w;
+  i64 u = p.u0 + threadIdx.x;
+  if (w.per_row == w.units) {      // one row: as in norm_groups
+    const i64 first = w.phase != 0, end = (w.width + w.phase) / W < p.u1 ? (w.width + w.phase) / W : p.u1;
+    if (u < first) u += THREADS;
+    for (; u < end; u += THREADS) {
+      const i64 e = u * W - w.phase;
+      step_group<ADAMW>(it, r, inv1, inv2, s, it.X + e, G + e, M + e, it.V + e, it.X16 + e, 0, W);
     }
-  } else {
-    for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) {
-      const i64 row = row_at(it.w, u), col = (u - row * it.w.cols) * W;
-      step_vector<ADAMW>(it, r, inv1, inv2, s, it.X + row * it.ldx + col, G + row * it.ldg + col, M + row * it.ldm + col, it.V + row * it.ldv + col, it.X16 + row * it.ldx16 + col);
-    }
+    u = threadIdx.x == 0 && p.u0 < first ? 0 : threadIdx.x == 32 && end >= first && end < p.u1 ? end : p.u1;
+  }
+  for (; u < p.u1; u += THREADS) {
+    const Spot at = group_at(w, u);
+    step_group<ADAMW>(it, r, inv1, inv2, s, it.X + at.row * it.ldx + at.col, G + at.row * it.ldg + at.col, M + at.row * it.ldm + at.col,
+                      it.V + at.row * it.ldv + at.col, it.X16 + at.row * it.ldx16 + at.col, at.lo, at.hi);
+    if (w.per_row == w.units) break;
   }
 }
 
 template <int CAP, bool ADAMW>
 __global__ void __launch_bounds__(THREADS, ADAMW ? ADAMW_RESIDENT : LION_RESIDENT) k_list_step(const __grid_constant__ Table<StepItem, CAP> t, const Rule r) {
   __shared__ float corr[2];
+  const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
+  i64 i = t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
   const float s = r.scale != nullptr ? *r.scale : 1.f;
   if (!isfinite(s)) {
@@ -531,26 +624,21 @@ __global__ void __launch_bounds__(THREADS, ADAMW ? ADAMW_RESIDENT : LION_RESIDEN
     __syncthreads();
     inv1 = corr[0]; inv2 = corr[1];
   }
-  const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
-  for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
+  for (i64 tile = t0; tile < t1; ++i) {
     const StepItem& it = t.item[i];
     i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
     if (end > t1) end = t1;
     if (end <= tile) continue;
     const Part p = part_of(it.w, tile, end);
-    if (it.w.kind == SINGLES) {
-      for (i64 e = p.u0 + threadIdx.x; e < p.u1; e += THREADS) {
-        const i64 row = row_at(it.w, e);
-        step_single<ADAMW>(it, r, inv1, inv2, s, row, e - row * it.w.cols);
-      }
-    } else if (it.g_bf16) {
-      if (it.m_bf16) step_vectors<ADAMW, __nv_bfloat16, __nv_bfloat16>(it, p, r, inv1, inv2, s);
-      else step_vectors<ADAMW, __nv_bfloat16, float>(it, p, r, inv1, inv2, s);
+    if (it.w.singles) {
+      step_singles<ADAMW>(it, p, r, inv1, inv2, s);
+    } else if (it.w.g_bf16) {
+      if (it.w.other_bf16) step_groups<ADAMW, __nv_bfloat16, __nv_bfloat16>(it, p, r, inv1, inv2, s);
+      else step_groups<ADAMW, __nv_bfloat16, float>(it, p, r, inv1, inv2, s);
     } else {
-      if (it.m_bf16) step_vectors<ADAMW, float, __nv_bfloat16>(it, p, r, inv1, inv2, s);
-      else step_vectors<ADAMW, float, float>(it, p, r, inv1, inv2, s);
+      if (it.w.other_bf16) step_groups<ADAMW, float, __nv_bfloat16>(it, p, r, inv1, inv2, s);
+      else step_groups<ADAMW, float, float>(it, p, r, inv1, inv2, s);
     }
-    ends_of(it.w, p, [&](i64 e) { step_single<ADAMW>(it, r, inv1, inv2, s, 0, e); });
     tile = end;
   }
 }

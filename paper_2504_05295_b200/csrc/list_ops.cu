@@ -18,19 +18,22 @@ namespace {
 // tiles a block, 1156 with 2; scaling 872M bf16 elements with their norm: 993 in one wave, 876, 785 and 794 with 4, 8 and 16;
 // Lion 717, 650 with 4 at four resident blocks; the norm alone does not care: 505 and 504).
 struct Shape {
-  int resident, tiles, most;      // blocks per SM of one wave, tiles per block beyond it, most blocks per SM
+  int resident, tiles;      // blocks per SM of one wave, tiles per block beyond it
+  i64 most;                 // blocks
 };
-constexpr Shape NORM_SHAPE = {NORM_RESIDENT, 8, 16}, SCALE_SHAPE = {SCALE_RESIDENT, 8, 1 << 20}, ADAMW_SHAPE = {ADAMW_RESIDENT, 4, 1 << 20},
-                LION_SHAPE = {LION_RESIDENT, 4, 1 << 20};
+constexpr i64 ANY = INT32_MAX;
+constexpr Shape NORM_SHAPE = {NORM_RESIDENT, INT32_MAX, MOST_NORM_BLOCKS}, SCALE_SHAPE = {SCALE_RESIDENT, 8, ANY},
+                ADAMW_SHAPE = {ADAMW_RESIDENT, 4, ANY}, LION_SHAPE = {LION_RESIDENT, 4, ANY};
 // Arrays in one launch: its parameters end at 32764 bytes.  Small lists take small parameters.
 constexpr int FEW = 24, SOME = 80;
-constexpr int MANY_NORM = 500, MANY_SCALE = 400, MANY_STEP = 236;
+constexpr int MANY_NORM = 500, MANY_SCALE = 400, MANY_STEP = 250;
 constexpr i64 MAX_ELEMENTS = (i64)1 << 50;      // (no element count or byte offset overflows)
 
 template <typename... KArgs, typename... Args>
 int launch(const Where& w, void (*kernel)(KArgs...), const Shape& shape, i64 tiles, const Args&... args) {
   i64 blocks = (i64)w.sm_count * shape.resident;
-  if (tiles / shape.tiles > blocks) blocks = std::min<i64>(tiles / shape.tiles, (i64)w.sm_count * shape.most);
+  if (tiles / shape.tiles > blocks) blocks = tiles / shape.tiles;
+  if (blocks > shape.most) blocks = shape.most;
   if (blocks > tiles) blocks = tiles;
   if (blocks < 1) blocks = 1;
   cudaLaunchConfig_t cfg = {};
@@ -141,40 +144,37 @@ struct Array {
 };
 inline int shift_of(int dtype) { return dtype == DION_BF16 ? 1 : 2; }
 
+constexpr i64 NARROW = 32;      // rows of fewer elements go one by one
+
 // How arrays of rows x cols are walked together, and their tiles behind the `tiles` so far.
 template <size_t N>
-Walk plan(i64 rows, i64 cols, const Array (&a)[N], i64* tiles) {
+Walk plan(i64 rows, i64 cols, int g_dtype, int other_dtype, const Array (&a)[N], i64* tiles) {
   Walk w = {};
-  w.n = rows * cols;
   w.first = *tiles;
-  if (w.n == 0) return w;
-  // the elements by which the addresses are beyond whole vectors, if they agree
-  int phase = -1;
-  bool agree = true, dense = true, vectors = cols % W == 0;
+  w.g_bf16 = g_dtype == DION_BF16; w.other_bf16 = other_dtype == DION_BF16;
+  if (rows == 0 || cols == 0) return w;
+  bool agree = true, dense = true;
+  int phase = -1, shift = 0;
   for (const Array& x : a) {
     if (x.p == nullptr) continue;
-    const int ph = (int)((uintptr_t)x.p >> x.shift) & (W - 1);
-    agree = agree && (phase < 0 || ph == phase);
-    phase = ph;
+    const int ph = (int)((uintptr_t)x.p >> x.shift) & (W - 1), sh = (int)x.ld & (W - 1);
+    agree = agree && (phase < 0 || (ph == phase && (rows == 1 || sh == shift)));
+    phase = ph; shift = sh;
     dense = dense && (rows == 1 || x.ld == cols);
-    vectors = vectors && ph == 0 && x.ld % W == 0;
   }
-  if (dense && agree) {
-    w.kind = DENSE;
-    w.head = (int)std::min<i64>((W - phase) % W, w.n);
-    w.units = (w.n - w.head) / W;
-    w.cols = w.units;
-  } else if (vectors) {
-    w.kind = SLICED;
-    w.units = w.n / W;
-    w.cols = cols / W;
+  if (dense) { cols *= rows; rows = 1; }
+  w.width = cols;
+  w.singles = !agree || (rows > 1 && cols < NARROW);
+  if (w.singles) {
+    w.per_row = cols;
   } else {
-    w.kind = SINGLES;
-    w.units = w.n;
-    w.cols = dense ? w.n : cols;
+    // (one row's first group starts at its phase; the rows of a matrix start at any)
+    w.per_row = rows == 1 ? (cols + phase + W - 1) / W : (cols + 2 * W - 2) / W;
+    w.phase = (uint8_t)phase; w.shift = (uint8_t)(rows == 1 ? 0 : shift);
   }
-  const i64 per = w.kind == SINGLES ? TILE_SINGLES : TILE_UNITS;
-  *tiles += std::max<i64>((w.units + per - 1) / per, 1);
+  w.units = rows * w.per_row;
+  const i64 per = w.singles ? THREADS * BATCH : TILE_UNITS;
+  *tiles += (w.units + per - 1) / per;
   return w;
 }
 
@@ -188,9 +188,9 @@ int norm_launches(const Where& w, const dion_grad* list, int count, bool inf, No
     for (int i = 0; i < t.count; ++i) {
       const dion_grad& a = list[done + i];
       NormItem* it = &t.item[i];
-      it->g = a.G; it->g_bf16 = a.g_dtype == DION_BF16; it->ldg = a.ldg;
+      it->g = a.G; it->ldg = a.ldg;
       const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}};
-      it->w = plan(a.rows, a.cols, arrays, &t.tiles);
+      it->w = plan(a.rows, a.cols, a.g_dtype, DION_F32, arrays, &t.tiles);
     }
     o.each = each != nullptr ? each + done : nullptr;
     o.use_carry = done > 0;
@@ -212,10 +212,10 @@ int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
     for (int i = 0; i < t.count; ++i) {
       const dion_grad& a = list[done + i];
       ScaleItem* it = &t.item[i];
-      it->g = a.G; it->g_bf16 = a.g_dtype == DION_BF16; it->ldg = a.ldg;
-      it->out = a.out; it->o_bf16 = a.out_dtype == DION_BF16; it->ldo = a.ldo;
+      it->g = a.G; it->ldg = a.ldg;
+      it->out = a.out; it->ldo = a.ldo;
       const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}, {a.out, a.ldo, shift_of(a.out_dtype)}};
-      it->w = plan(a.rows, a.cols, arrays, &t.tiles);
+      it->w = plan(a.rows, a.cols, a.g_dtype, a.out_dtype, arrays, &t.tiles);
     }
     done += t.count;
     LIST_TRY(launch(w, k_list_scale<CAP>, SCALE_SHAPE, t.tiles, t, c));
@@ -235,14 +235,14 @@ int step_launches(const Where& w, const dion_param* list, int count, Rule r, flo
       const dion_param& a = list[done + i];
       StepItem* it = &t.item[i];
       it->X = (float*)a.X; it->ldx = a.ldx;
-      it->G = a.G; it->ldg = a.ldg; it->g_bf16 = a.g_dtype == DION_BF16;
-      it->M = a.M; it->ldm = a.ldm; it->m_bf16 = a.m_dtype == DION_BF16;
+      it->G = a.G; it->ldg = a.ldg;
+      it->M = a.M; it->ldm = a.ldm;
       it->V = ADAMW ? (float*)a.V : nullptr; it->ldv = a.ldv;
       it->X16 = (__nv_bfloat16*)a.X16; it->ldx16 = a.ldx16;
       it->lr = lr * a.lr_scale;
       it->keep = (float)(1.0 - (double)lr * a.lr_scale * a.weight_decay);
       const Array arrays[] = {{it->X, a.ldx, 2}, {a.G, a.ldg, shift_of(a.g_dtype)}, {a.M, a.ldm, shift_of(a.m_dtype)}, {it->V, a.ldv, 2}, {it->X16, a.ldx16, 1}};
-      it->w = plan(a.rows, a.cols, arrays, &t.tiles);
+      it->w = plan(a.rows, a.cols, a.g_dtype, a.m_dtype, arrays, &t.tiles);
     }
     r.first = done == 0;
     done += t.count;
@@ -266,7 +266,8 @@ bool load(K kernel) {
 
 }  // namespace
 
-size_t scratch_bytes(int sm_count) { return sizeof(Scratch) + sizeof(double) * ((size_t)sm_count * NORM_SHAPE.most + MANY_NORM); }
+size_t scratch_bytes() { return sizeof(Scratch); }
+static_assert(MANY_NORM <= MOST_PARTS - MOST_NORM_BLOCKS, "a launch's partial results fit");
 
 int configure() {
   const bool ok = load(k_list_norm<SOME, false>) && load(k_list_norm<SOME, true>) && load(k_list_scale<SOME>) && load(k_list_step<SOME, false>) &&
