@@ -15,6 +15,7 @@ namespace list {
 constexpr int THREADS = 256;
 constexpr int NORM_RESIDENT = 4, SCALE_RESIDENT = 4, ADAMW_RESIDENT = 3, LION_RESIDENT = 4;      // blocks per SM
 constexpr int MOST_NORM_BLOCKS = 1024, MOST_PARTS = MOST_NORM_BLOCKS + 500;      // blocks of a norm launch; with its arrays
+constexpr int FEW_PARTS = 8;         // partial results of an array that one thread adds up
 constexpr int TILE_UNITS = 256;      // groups of a tile, one per thread
 constexpr int BATCH = 4;             // elements that a thread takes at once from an array that is walked one by one
 constexpr int W = 8;                 // elements of a group: 32 bytes of fp32 (one load on sm_100), 16 of bf16
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
   __shared__ double red[THREADS / 32];
   __shared__ bool last;
   __shared__ double parts[MOST_PARTS];
-  __shared__ i64 starts[CAP + 1];
+  __shared__ int from[CAP], upto[CAP];
   const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
   i64 i = t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
@@ -356,18 +357,26 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
   __threadfence();
   Acc<INF> all;
   if (each) {
-    // every partial result in one round trip; then a warp per array, whose first and last block are those that own its
-    // first and last tile
+    // Every partial result in one round trip.  Those of array i begin with the block that owns its first tile and end with the one
+    // that owns its last; a thread adds up a few, a warp many.
     for (int k = threadIdx.x; k < G + t.count; k += THREADS) parts[k] = __ldcg(&s->part[k]);
-    for (int i = threadIdx.x; i <= t.count; i += THREADS) starts[i] = i < t.count ? t.item[i].w.first : t.tiles;
+    for (int i = threadIdx.x; i < t.count; i += THREADS) {
+      const i64 f = t.item[i].w.first, l = (i + 1 < t.count ? t.item[i + 1].w.first : t.tiles) - 1;
+      from[i] = f <= l ? (int)(((f + 1) * G - 1) / t.tiles) + i : 0;
+      upto[i] = f <= l ? (int)(((l + 1) * G - 1) / t.tiles) + i + 1 : 0;
+    }
     __syncthreads();
-    for (int i = threadIdx.x >> 5; i < t.count; i += THREADS / 32) {
-      const i64 f = starts[i], l = starts[i + 1] - 1;
+    for (int i = threadIdx.x; i < t.count; i += THREADS) {
+      if (upto[i] - from[i] > FEW_PARTS) continue;
       Acc<INF> a;
-      if (f <= l) {
-        const i64 b0 = ((f + 1) * G - 1) / t.tiles, b1 = ((l + 1) * G - 1) / t.tiles;
-        for (i64 b = b0 + (threadIdx.x & 31); b <= b1; b += 32) a.merge(parts[b + i]);
-      }
+      for (int k = from[i]; k < upto[i]; ++k) a.merge(parts[k]);
+      o.each[i] = a.norm();
+      all.merge(a.kept());
+    }
+    for (int i = threadIdx.x >> 5; i < t.count; i += THREADS / 32) {
+      if (upto[i] - from[i] <= FEW_PARTS) continue;
+      Acc<INF> a;
+      for (int k = from[i] + (threadIdx.x & 31); k < upto[i]; k += 32) a.merge(parts[k]);
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) {
         if (INF) a.m = max(a.m, __shfl_xor_sync(0xffffffffu, a.m, d));

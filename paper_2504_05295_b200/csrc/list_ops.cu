@@ -51,7 +51,7 @@ inline int bytes_of(int dtype) { return dtype == DION_BF16 ? 2 : 4; }
 inline bool known_type(int dtype) { return dtype == DION_F32 || dtype == DION_BF16; }
 
 // rows x cols elements, or a refusal
-bool too_many(i64 a, i64 b) { return (unsigned __int128)a * (unsigned __int128)b > (unsigned __int128)MAX_ELEMENTS; }
+bool too_many(i64 a, i64 b) { return ((a | b) >> 25) != 0 && (unsigned __int128)a * (unsigned __int128)b > (unsigned __int128)MAX_ELEMENTS; }
 int check_shape(i64 rows, i64 cols) {
   return rows < 0 || cols < 0 || rows > MAX_ELEMENTS || cols > MAX_ELEMENTS || too_many(rows, cols) ? DION_ERR_SHAPE : DION_OK;
 }
@@ -88,29 +88,39 @@ bool conflict(const Range& a, const Range& b) {
   return true;
 }
 
-// Whether anything that a call writes is touched twice.  The ranges come kind by kind (all X, all G, ...), and lists are often
-// views of a few buffers in ascending order: a few runs of ranges that lie one behind the other, and apart from the other runs,
-// need no sorting (65 parameters: 5 us).  `each(f)` calls f(pointer, rows, cols, ld, size, written) for every range.
-template <class Each>
-int check_ranges(const Each& each) {
-  constexpr int MOST = 8;
+// Ranges of one kind (all X, all G, ...).  Lists are often views of a few buffers in ascending order: a few runs of ranges that lie
+// one behind the other.
+struct Runs {
+  static constexpr int MOST = 4;
   uintptr_t begin[MOST], end[MOST];
-  int runs = 0;
-  size_t n = 0;
-  each([&](const void* p, i64 rows, i64 cols, i64 ld, int size, bool written) {
+  int n = 0;
+  void add(const void* p, i64 rows, i64 cols, i64 ld, int size) {
     if (p == nullptr || rows == 0 || cols == 0) return;
-    const Range r = range_of(p, rows, cols, ld, size, written);
-    ++n;
-    if (runs > MOST) return;
-    if (runs > 0 && r.begin >= end[runs - 1]) { end[runs - 1] = r.end; return; }
-    if (runs == MOST) { ++runs; return; }
-    begin[runs] = r.begin;
-    end[runs++] = r.end;
-  });
-  bool apart = runs <= MOST;
-  for (int a = 0; apart && a < runs; ++a)
-    for (int b = a + 1; b < runs; ++b) apart = apart && (begin[a] >= end[b] || begin[b] >= end[a]);
+    const uintptr_t b = (uintptr_t)p, e = b + (uintptr_t)((rows - 1) * ld + cols) * (uintptr_t)size;
+    if (n > 0 && n <= MOST && b >= end[n - 1]) { end[n - 1] = e; return; }
+    if (n < MOST) { begin[n] = b; end[n] = e; }
+    if (n <= MOST) ++n;
+  }
+};
+
+// Whether anything that a call writes is touched twice.  Runs that lie apart need no look at their ranges (65 parameters: 5 us
+// of sorting); else `each(f)` calls f(pointer, rows, cols, ld, size, written) for every range.
+template <int KINDS, class Each>
+int check_ranges(const Runs (&kind)[KINDS], const Each& each) {
+  uintptr_t begin[KINDS * Runs::MOST], end[KINDS * Runs::MOST];
+  int runs = 0;
+  bool apart = true;
+  for (const Runs& k : kind) {
+    if (k.n > Runs::MOST) { apart = false; break; }
+    for (int i = 0; i < k.n; ++i) {
+      for (int j = 0; j < runs; ++j) apart = apart && (begin[j] >= k.end[i] || k.begin[i] >= end[j]);
+      begin[runs] = k.begin[i];
+      end[runs++] = k.end[i];
+    }
+  }
   if (apart) return DION_OK;
+  size_t n = 0;
+  each([&](const void* p, i64 rows, i64 cols, i64, int, bool) { n += p != nullptr && rows != 0 && cols != 0; });
   Range* r = new (std::nothrow) Range[n];
   if (r == nullptr) return DION_ERR_NOMEM;
   n = 0;
@@ -178,24 +188,63 @@ Walk plan(i64 rows, i64 cols, int g_dtype, int other_dtype, const Array (&a)[N],
   return w;
 }
 
+// Whether arrays that lie one behind the other can be walked as one: dense, of the same types, each where the one before it ends.
+// Parameters and gradients are often views of flat buffers; 65 neighbours are one item instead of a table of 65 (AdamW, host
+// time: 7.9 -> 5.5 us).
+bool follows(const void* a, const void* b, i64 n, int size) { return (uintptr_t)b == (uintptr_t)a + (uintptr_t)(n * size); }
+bool dense(const dion_grad& a, bool out) { return a.rows == 1 || (a.ldg == a.cols && (!out || a.ldo == a.cols)); }
+bool continues(const dion_grad& a, const dion_grad& b, bool out) {
+  const i64 n = a.rows * a.cols;
+  return n > 0 && b.rows > 0 && b.cols > 0 && a.g_dtype == b.g_dtype && follows(a.G, b.G, n, bytes_of(a.g_dtype)) && dense(a, out) && dense(b, out) &&
+         (!out || (a.out_dtype == b.out_dtype && follows(a.out, b.out, n, bytes_of(a.out_dtype))));
+}
+bool dense(const dion_param& a, bool v) {
+  return a.rows == 1 || (a.ldx == a.cols && a.ldg == a.cols && a.ldm == a.cols && (!v || a.ldv == a.cols) && (a.X16 == nullptr || a.ldx16 == a.cols));
+}
+bool continues(const dion_param& a, const dion_param& b, bool v) {
+  const i64 n = a.rows * a.cols;
+  return n > 0 && b.rows > 0 && b.cols > 0 && follows(a.X, b.X, n, 4) && a.g_dtype == b.g_dtype && follows(a.G, b.G, n, bytes_of(a.g_dtype)) &&
+         a.m_dtype == b.m_dtype && follows(a.M, b.M, n, bytes_of(a.m_dtype)) && (!v || follows(a.V, b.V, n, 4)) &&
+         (a.X16 == nullptr ? b.X16 == nullptr : follows(a.X16, b.X16, n, 2)) && a.lr_scale == b.lr_scale && a.weight_decay == b.weight_decay &&
+         dense(a, v) && dense(b, v);
+}
+template <class D>
+int items_of(const D* list, int count, bool more) {
+  int n = count > 0;
+  for (int i = 1; i < count; ++i) n += !continues(list[i - 1], list[i], more);
+  return n;
+}
+// The array at list[*at] with all that continue it, as one; *at is then behind them.
+template <class D>
+void take(const D* list, int count, bool more, int* at, i64* rows, i64* cols) {
+  int i = *at;
+  *rows = list[i].rows; *cols = list[i].cols;
+  for (; i + 1 < count && continues(list[i], list[i + 1], more); ++i) {
+    *cols = *rows * *cols + list[i + 1].rows * list[i + 1].cols;
+    *rows = 1;
+  }
+  *at = i + 1;
+}
+
 template <int CAP>
 int norm_launches(const Where& w, const dion_grad* list, int count, bool inf, NormOut o, float* each) {
   Table<NormItem, CAP> t;
   int done = 0;
   do {
     t.tiles = 0;
-    t.count = std::min(count - done, CAP);
-    for (int i = 0; i < t.count; ++i) {
-      const dion_grad& a = list[done + i];
-      NormItem* it = &t.item[i];
-      it->g = a.G; it->ldg = a.ldg;
-      const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}};
-      it->w = plan(a.rows, a.cols, a.g_dtype, DION_F32, arrays, &t.tiles);
-    }
+    t.count = 0;
     o.each = each != nullptr ? each + done : nullptr;
     o.use_carry = done > 0;
-    o.last = done + t.count == count;
-    done += t.count;
+    while (done < count && t.count < CAP) {
+      const dion_grad& a = list[done];
+      NormItem* it = &t.item[t.count++];
+      i64 rows = a.rows, cols = a.cols;
+      if (each != nullptr) ++done; else take(list, count, false, &done, &rows, &cols);
+      it->g = a.G; it->ldg = a.ldg;
+      const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}};
+      it->w = plan(rows, cols, a.g_dtype, DION_F32, arrays, &t.tiles);
+    }
+    o.last = done == count;
     if (inf) LIST_TRY(launch(w, k_list_norm<CAP, true>, NORM_SHAPE, t.tiles, t, o));
     else LIST_TRY(launch(w, k_list_norm<CAP, false>, NORM_SHAPE, t.tiles, t, o));
   } while (done < count);
@@ -208,16 +257,17 @@ int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
   int done = 0;
   do {
     t.tiles = 0;
-    t.count = std::min(count - done, CAP);
-    for (int i = 0; i < t.count; ++i) {
-      const dion_grad& a = list[done + i];
-      ScaleItem* it = &t.item[i];
+    t.count = 0;
+    while (done < count && t.count < CAP) {
+      const dion_grad& a = list[done];
+      ScaleItem* it = &t.item[t.count++];
+      i64 rows, cols;
+      take(list, count, true, &done, &rows, &cols);
       it->g = a.G; it->ldg = a.ldg;
       it->out = a.out; it->ldo = a.ldo;
       const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}, {a.out, a.ldo, shift_of(a.out_dtype)}};
-      it->w = plan(a.rows, a.cols, a.g_dtype, a.out_dtype, arrays, &t.tiles);
+      it->w = plan(rows, cols, a.g_dtype, a.out_dtype, arrays, &t.tiles);
     }
-    done += t.count;
     LIST_TRY(launch(w, k_list_scale<CAP>, SCALE_SHAPE, t.tiles, t, c));
     c.norm_out = nullptr; c.coef_out = nullptr;
   } while (done < count);
@@ -230,10 +280,13 @@ int step_launches(const Where& w, const dion_param* list, int count, Rule r, flo
   int done = 0;
   while (done < count) {
     t.tiles = 0;
-    t.count = std::min(count - done, CAP);
-    for (int i = 0; i < t.count; ++i) {
-      const dion_param& a = list[done + i];
-      StepItem* it = &t.item[i];
+    t.count = 0;
+    r.first = done == 0;
+    while (done < count && t.count < CAP) {
+      const dion_param& a = list[done];
+      StepItem* it = &t.item[t.count++];
+      i64 rows, cols;
+      take(list, count, ADAMW, &done, &rows, &cols);
       it->X = (float*)a.X; it->ldx = a.ldx;
       it->G = a.G; it->ldg = a.ldg;
       it->M = a.M; it->ldm = a.ldm;
@@ -242,10 +295,8 @@ int step_launches(const Where& w, const dion_param* list, int count, Rule r, flo
       it->lr = lr * a.lr_scale;
       it->keep = (float)(1.0 - (double)lr * a.lr_scale * a.weight_decay);
       const Array arrays[] = {{it->X, a.ldx, 2}, {a.G, a.ldg, shift_of(a.g_dtype)}, {a.M, a.ldm, shift_of(a.m_dtype)}, {it->V, a.ldv, 2}, {it->X16, a.ldx16, 1}};
-      it->w = plan(a.rows, a.cols, a.g_dtype, a.m_dtype, arrays, &t.tiles);
+      it->w = plan(rows, cols, a.g_dtype, a.m_dtype, arrays, &t.tiles);
     }
-    r.first = done == 0;
-    done += t.count;
     LIST_TRY(launch(w, k_list_step<CAP, ADAMW>, ADAMW ? ADAMW_SHAPE : LION_SHAPE, t.tiles, t, r));
   }
   return DION_OK;
@@ -253,7 +304,8 @@ int step_launches(const Where& w, const dion_param* list, int count, Rule r, flo
 
 template <bool ADAMW>
 int step(const Where& w, const dion_param* list, int count, const Rule& r, float lr) {
-  return count <= FEW ? step_launches<FEW, ADAMW>(w, list, count, r, lr) : count <= SOME ? step_launches<SOME, ADAMW>(w, list, count, r, lr)
+  const int items = items_of(list, count, ADAMW);
+  return items <= FEW ? step_launches<FEW, ADAMW>(w, list, count, r, lr) : items <= SOME ? step_launches<SOME, ADAMW>(w, list, count, r, lr)
                       : step_launches<MANY_STEP, ADAMW>(w, list, count, r, lr);
 }
 
@@ -311,18 +363,24 @@ int check_clip(const dion_grad* list, int count, float max_norm, int norm_type, 
   LIST_TRY(check_floats(norms));
   LIST_TRY(check_floats(norm_out));
   LIST_TRY(check_floats(coef_out));
+  const auto in_place = [](const dion_grad& a) { return a.G == a.out && a.g_dtype == a.out_dtype && (a.ldg == a.ldo || a.rows <= 1); };
+  Runs kind[5];
   for (int i = 0; i < count; ++i) {
     const dion_grad& a = list[i];
     if (!known_type(a.g_dtype) || !known_type(a.out_dtype)) return DION_ERR_INVALID;
     LIST_TRY(check_shape(a.rows, a.cols));
     LIST_TRY(check_array(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype)));
     LIST_TRY(check_array(a.out, a.rows, a.cols, a.ldo, bytes_of(a.out_dtype)));
+    if (!in_place(a)) kind[0].add(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype));
+    kind[1].add(a.out, a.rows, a.cols, a.ldo, bytes_of(a.out_dtype));
   }
-  return check_ranges([&](auto range) {
+  kind[2].add(norms, 1, num_norms, num_norms, 4);
+  kind[3].add(norm_out, 1, 1, 1, 4);
+  kind[4].add(coef_out, 1, 1, 1, 4);
+  return check_ranges(kind, [&](auto range) {
     for (int i = 0; i < count; ++i) {
       const dion_grad& a = list[i];
-      const bool in_place = a.G == a.out && a.g_dtype == a.out_dtype && (a.ldg == a.ldo || a.rows <= 1);
-      if (!in_place) range(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype), false);
+      if (!in_place(a)) range(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype), false);
     }
     for (int i = 0; i < count; ++i) range(list[i].out, list[i].rows, list[i].cols, list[i].ldo, bytes_of(list[i].out_dtype), true);
     range(norms, 1, num_norms, num_norms, 4, false);
@@ -337,6 +395,7 @@ int check_step(bool adamw, const dion_param* list, int count, const dion_rule* r
   if (adamw && (!(rule->eps >= 0.0) || !isfinite(rule->eps) || (rule->step_dev == nullptr && rule->step < 1))) return DION_ERR_INVALID;
   if ((uintptr_t)rule->step_dev & 7) return DION_ERR_ALIGN;
   LIST_TRY(check_floats(rule->grad_scale));
+  Runs kind[7];
   for (int i = 0; i < count; ++i) {
     const dion_param& a = list[i];
     if (!known_type(a.g_dtype) || !known_type(a.m_dtype) || !isfinite(a.lr_scale) || !isfinite(a.weight_decay)) return DION_ERR_INVALID;
@@ -346,8 +405,15 @@ int check_step(bool adamw, const dion_param* list, int count, const dion_rule* r
     LIST_TRY(check_array(a.M, a.rows, a.cols, a.ldm, bytes_of(a.m_dtype)));
     if (adamw) LIST_TRY(check_array(a.V, a.rows, a.cols, a.ldv, 4));
     if (a.X16 != nullptr) LIST_TRY(check_array(a.X16, a.rows, a.cols, a.ldx16, 2));
+    kind[0].add(a.X, a.rows, a.cols, a.ldx, 4);
+    kind[1].add(a.G, a.rows, a.cols, a.ldg, bytes_of(a.g_dtype));
+    kind[2].add(a.M, a.rows, a.cols, a.ldm, bytes_of(a.m_dtype));
+    if (adamw) kind[3].add(a.V, a.rows, a.cols, a.ldv, 4);
+    kind[4].add(a.X16, a.rows, a.cols, a.ldx16, 2);
   }
-  return check_ranges([&](auto range) {
+  if (adamw) kind[5].add(rule->step_dev, 1, 1, 1, 8);
+  kind[6].add(rule->grad_scale, 1, 1, 1, 4);
+  return check_ranges(kind, [&](auto range) {
     for (int i = 0; i < count; ++i) range(list[i].X, list[i].rows, list[i].cols, list[i].ldx, 4, true);
     for (int i = 0; i < count; ++i) range(list[i].G, list[i].rows, list[i].cols, list[i].ldg, bytes_of(list[i].g_dtype), false);
     for (int i = 0; i < count; ++i) range(list[i].M, list[i].rows, list[i].cols, list[i].ldm, bytes_of(list[i].m_dtype), true);
@@ -365,7 +431,8 @@ int grad_norm(const Where& w, const dion_grad* list, int count, int norm_type, f
   o.norm = norm_out; o.coef = coef_out; o.max_norm = max_norm;
   o.status = w.status;
   const bool inf = norm_type == DION_NORM_INF;
-  return count <= FEW ? norm_launches<FEW>(w, list, count, inf, o, each_out) : count <= SOME ? norm_launches<SOME>(w, list, count, inf, o, each_out)
+  const int items = each_out != nullptr ? count : items_of(list, count, false);
+  return items <= FEW ? norm_launches<FEW>(w, list, count, inf, o, each_out) : items <= SOME ? norm_launches<SOME>(w, list, count, inf, o, each_out)
                       : norm_launches<MANY_NORM>(w, list, count, inf, o, each_out);
 }
 
@@ -381,7 +448,8 @@ int clip_grads(const Where& w, const dion_grad* list, int count, float max_norm,
     if (count == 0) return DION_OK;
     c.coef = &((Scratch*)w.scratch)->coef;
   }
-  return count <= FEW ? scale_launches<FEW>(w, list, count, c) : count <= SOME ? scale_launches<SOME>(w, list, count, c)
+  const int items = items_of(list, count, true);
+  return items <= FEW ? scale_launches<FEW>(w, list, count, c) : items <= SOME ? scale_launches<SOME>(w, list, count, c)
                       : scale_launches<MANY_SCALE>(w, list, count, c);
 }
 
