@@ -204,6 +204,75 @@ def test_clip(opt, types, lie):
     assert opt.get_status() == (0, 0)
 
 
+@pytest.mark.parametrize("kind", [2, "inf"])
+@pytest.mark.parametrize("lie", [PLAIN, SHIFTED, SLICED, ALIGNED_SLICES])
+@pytest.mark.parametrize("types", ["f32 bf16", "bf16 f32", "f32 in place", "bf16 in place"])
+def test_clip_short_lists(opt, types, lie, kind):
+    # lists that one launch clips, up to its last tile and just beyond
+    src, dst = types.split(" ", 1)
+    for shapes in ([(1, 1)], SHAPES[:16], [(1, 262144)], [(64, 2048), (64, 2048)], [(1, 262145)], [(3, 40)] * 60, [(2, 40)] * 90, [(0, 5), (1, 3)]):
+        ts = [place(s, DT[src], lie, seed=k) for k, s in enumerate(shapes)]
+        grads = [t for t, _ in ts]
+        before = [g.clone() for g in grads]
+        outs = ts if dst == "in place" else [place(s, DT[dst], lie, value=3.0, seed=k) for k, s in enumerate(shapes)]
+        want = norm64(grads, kind)
+        norm, coef, alone = scalar(), scalar(), scalar()
+        items = binding.grad_list(grads, None if dst == "in place" else [o for o, _ in outs])
+        opt.grad_norm(items, kind, norm_out=alone)
+        opt.clip_grads(items, 0.25 * want, norm_type=kind, norm_out=norm, coef_out=coef)
+        tol = NORM if kind == 2 else 0.0
+        assert abs(float(norm) - want) <= tol * want and abs(float(alone) - want) <= tol * want
+        assert abs(float(coef) - 0.25) <= (COEF + u) * 0.25
+        check_clipped(grads, [o for o, _ in outs], before, 0.25)
+        for o, buf in outs + ts:
+            assert surroundings_kept(o, buf)
+    assert opt.get_status() == (0, 0)
+
+
+def test_neighbours_in_memory(opt):
+    # views of flat buffers, one behind the other, with what must not be walked as one: a gap, another type, another
+    # rate, another decay, a slice, an empty array
+    sizes = [5, 8, 4096, 1, 333, 64, 0, 77, 2048, 9, 1000]
+    total = sum(sizes)
+    flat = {k: torch.randn(total + 1, generator=gen(i), device="cuda") for i, k in enumerate(("X", "G", "M"))}
+    flat["V"] = torch.rand(total + 1, generator=gen(9), device="cuda")
+    flat["X16"] = torch.zeros(total + 1, dtype=torch.bfloat16, device="cuda")
+    at, views = 0, []
+    for n in sizes:
+        views.append({k: f[at:at + n] for k, f in flat.items()})
+        at += n
+    views[3]["G"] = views[3]["G"].bfloat16()
+    scales = [1.0] * 4 + [0.5] * 7
+    decays = [0.0] * 8 + [0.25] * 3
+    for adamw in (True, False):
+        before = [{k: t.clone() for k, t in v.items()} for v in views]
+        tail = {k: f[-1].clone() for k, f in flat.items()}
+        params = binding.param_list([binding.param_desc(v["X"], v["G"], v["M"], v["V"] if adamw else None, v["X16"], s, d)
+                                     for v, s, d in zip(views, scales, decays)])
+        if adamw:
+            opt.adamw_step(params, 0.01, 2)
+        else:
+            opt.lion_step(params, 0.01, 0.9, 0.95)
+        for b, v, s, d in zip(before, views, scales, decays):
+            check_step(b, v, adamw, f32(0.01), 0.9, 0.95, 1e-8, 2, 1.0, s, d)
+        assert all(torch.equal(f[-1], tail[k]) for k, f in flat.items())
+    # the norm and the scaling of the same views, some left out
+    for left_out in ([], [2], [0, 5]):
+        gs = [v["G"] for k, v in enumerate(views) if k not in left_out]
+        G = flat["G"].clone()
+        outs = [torch.zeros_like(g) for g in gs]
+        norm, coef = scalar(), scalar()
+        opt.clip_grads(binding.grad_list(gs, outs), 1.0, norm_out=norm, coef_out=coef)
+        want = norm64(gs)
+        assert abs(float(norm) - want) <= NORM * want
+        check_clipped(gs, outs, gs, 1.0 / want)
+        opt.clip_grads(binding.grad_list(gs), 1e9, norm_out=norm)
+        assert abs(float(norm) - want) <= NORM * want and torch.equal(G, flat["G"])
+    opt.clip_grads(binding.grad_list([v["G"] for k, v in enumerate(views) if k not in (2, 3)]), 0.0)
+    assert not any(bool(v["G"].any()) for k, v in enumerate(views) if k not in (2, 3))
+    assert torch.equal(flat["G"][13:13 + 4097], G[13:13 + 4097]) and torch.equal(flat["G"][-1], G[-1])
+
+
 def test_clip_below_the_threshold(opt):
     ts = [torch.randn(s, generator=gen(3), device="cuda") for s in ((100, 33), (4097,))]
     before = [t.clone() for t in ts]
