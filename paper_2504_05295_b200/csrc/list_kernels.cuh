@@ -622,6 +622,15 @@ __device__ __forceinline__ float lion_sign(const Rule& r, float m, float g, floa
   return c > 0.f ? 1.f : c < 0.f ? -1.f : c;      // (a NaN stays one)
 }
 
+// The update's root and quotient need not be the nearest numbers (relative errors 2^-23 and 2^-22, of an update that is a
+// thousandth of X or so); the correctly rounded ones are most of a short list's instructions (65 odd slices 11.9 us against 8.2).
+// (Divisors: below 2^-126 only as zero, where the quotient is that of zero, and never near 2^126.)
+__device__ __forceinline__ float sqrt_approx(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // One element's step.  m is the new moment before it is rounded to the array's type: only what is kept is rounded.
 template <bool ADAMW>
 __device__ __forceinline__ void step_element(const Rule& r, float inv1, float inv2, float s, float lr, float keep, float& x, float& m, float& v, float g) {
@@ -629,7 +638,7 @@ __device__ __forceinline__ void step_element(const Rule& r, float inv1, float in
     g *= s;
     m = fmaf(r.b1, m, r.c1 * g);
     v = fmaf(r.b2, v, r.c2 * (g * g));
-    x = fmaf(-lr, (m * inv1) / (sqrtf(v * inv2) + r.eps), x * keep);
+    x = fmaf(-lr, __fdividef(m * inv1, sqrt_approx(v * inv2) + r.eps), x * keep);
   } else {
     x = fmaf(-lr, lion_sign(r, m, g, s), x * keep);
     m = fmaf(r.b2, m, r.c2 * (s * g));

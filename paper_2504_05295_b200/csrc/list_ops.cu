@@ -95,35 +95,64 @@ bool conflict(const Range& a, const Range& b) {
   return true;
 }
 
-// Ranges of one kind (all X, all G, ...).  Lists are often views of a few buffers in ascending order: a few runs of ranges that lie
-// one behind the other.
-struct Runs {
-  static constexpr int MOST = 4;
-  uintptr_t begin[MOST], end[MOST];
-  int n = 0;
+// Ranges of one kind (all X, all G, ...), as runs of ranges that follow one another at once or after a short gap: lists are often
+// views of a few buffers.
+struct Run {
+  uintptr_t begin, end;
+};
+class Runs {
+ public:
+  ~Runs() { if (run != few) delete[] run; }
   void add(const void* p, i64 rows, i64 cols, i64 ld, int size) {
     if (p == nullptr || rows == 0 || cols == 0) return;
     const uintptr_t b = (uintptr_t)p, e = b + (uintptr_t)((rows - 1) * ld + cols) * (uintptr_t)size;
-    if (n > 0 && n <= MOST && b >= end[n - 1]) { end[n - 1] = e; return; }
-    if (n < MOST) { begin[n] = b; end[n] = e; }
-    if (n <= MOST) ++n;
+    if (n > 0 && b >= run[n - 1].end && b - run[n - 1].end <= GAP) { run[n - 1].end = e; return; }
+    if (n == cap && !grow()) return;
+    sorted = sorted && (n == 0 || b >= run[n - 1].begin);
+    run[n++] = {b, e};
   }
+  void sort() {
+    if (!sorted) std::sort(run, run + n, [](const Run& a, const Run& b) { return a.begin < b.begin; });
+  }
+  Run* run = few;
+  int n = 0;
+  bool no_memory = false;
+
+ private:
+  static constexpr uintptr_t GAP = 4096;
+  bool grow() {
+    Run* more = new (std::nothrow) Run[2 * (size_t)cap];
+    if (more == nullptr) { no_memory = true; return false; }
+    std::copy(run, run + n, more);
+    if (run != few) delete[] run;
+    run = more;
+    cap *= 2;
+    return true;
+  }
+  Run few[16];
+  int cap = 16;
+  bool sorted = true;
 };
 
-// Whether anything that a call writes is touched twice.  Runs that lie apart need no look at their ranges (65 parameters: 5 us
-// of sorting); else `each(f)` calls f(pointer, rows, cols, ld, size, written) for every range.
+// Whether anything that a call writes is touched twice.  The kinds' runs are looked through side by side; where two of them meet,
+// `each(f)` calls f(pointer, rows, cols, ld, size, written) for every range, and these are sorted and compared one by one.
 template <int KINDS, class Each>
-int check_ranges(const Runs (&kind)[KINDS], const Each& each) {
-  uintptr_t begin[KINDS * Runs::MOST], end[KINDS * Runs::MOST];
-  int runs = 0;
+int check_ranges(Runs (&kind)[KINDS], const Each& each) {
+  int at[KINDS] = {};
   bool apart = true;
-  for (const Runs& k : kind) {
-    if (k.n > Runs::MOST) { apart = false; break; }
-    for (int i = 0; i < k.n; ++i) {
-      for (int j = 0; j < runs; ++j) apart = apart && (begin[j] >= k.end[i] || k.begin[i] >= end[j]);
-      begin[runs] = k.begin[i];
-      end[runs++] = k.end[i];
-    }
+  uintptr_t end = 0;
+  for (Runs& k : kind) {
+    if (k.no_memory) return DION_ERR_NOMEM;
+    k.sort();
+  }
+  for (;;) {
+    int first = -1;
+    for (int k = 0; k < KINDS; ++k)
+      if (at[k] < kind[k].n && (first < 0 || kind[k].run[at[k]].begin < kind[first].run[at[first]].begin)) first = k;
+    if (first < 0) break;
+    const Run& r = kind[first].run[at[first]++];
+    if (r.begin < end) { apart = false; break; }
+    end = r.end;
   }
   if (apart) return DION_OK;
   size_t n = 0;

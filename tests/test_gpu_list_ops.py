@@ -389,11 +389,12 @@ def check_step(before, after, adamw, lr, b1, b2, eps, t, s, lr_scale, wd):
         step = new_m / (1 - b1 ** t) / den
         size_m = b1 * m.abs() + (1 - b1) * g.abs()
         # M: beta, 1 - beta, s g, the product and the sum, one rounding each.  V: those of the square too, all its terms
-        # positive; squares below 2^-126 lose what is below 2^-149.  The step: M's error, V's halved by the root, the two
-        # corrections, product, root, sum, quotient.
+        # positive; squares below 2^-126 lose what is below 2^-149.  The step: M's error and, relative to the step, V's
+        # 6 u halved by the root (3), V's correction and its product halved (1), the root 2^-23 (2), eps and the sum (2), M's
+        # correction and its product (2), the quotient 2^-22 (4): 14 u.
         tol_m, tol_v = 5 * u * size_m + TINY, 8 * u * new_v + 4 * TINY
         # (sqrt(V + tiny) - sqrt(V) <= sqrt(tiny): counts where V itself is that small)
-        tol_step = 5 * u * size_m / (1 - b1 ** t) / den + 12 * u * step.abs() + step.abs() * torch.sqrt(torch.full_like(den, 4 * TINY)) / den
+        tol_step = 5 * u * size_m / (1 - b1 ** t) / den + 14 * u * step.abs() + step.abs() * torch.sqrt(torch.full_like(den, 4 * TINY)) / den
         assert bool(((after["V"].double() - new_v).abs() <= tol_v).all())
     else:
         c = b1 * m + (1 - b1) * g
