@@ -138,7 +138,8 @@ enum {
                                  fallback could not cure either): the step that saw it left
                                  X, M and Q unchanged                              */
   DION_STATUS_NONFINITE = 2,  /* NaN or Inf in M, G or Q (seen in the trace of the panel's Gram
-                                 matrix: the step is cancelled), or in a column norm of R */
+                                 matrix: the step is cancelled), or in a column norm of R;
+                                 a gradient norm or a grad_scale that is not finite */
   DION_STATUS_TIMEOUT = 4,    /* a bounded device-side wait ran out                */
   DION_STATUS_ILLCOND = 8     /* the adaptive rounds ran out before the panel was seen
                                  well conditioned; the result may be less accurate  */
@@ -311,7 +312,7 @@ typedef struct {
  *   each_out   `count` norms, one per array
  *   coef_out   min(1, max_norm / norm), what dion_clip_grads would multiply by, for dion_rule.grad_scale (max_norm >= 0, may be
  *              infinite; ignored without coef_out)
- * A norm that is not finite sets DION_STATUS_NONFINITE, and the coefficient is NaN. */
+ * A norm that is not finite (or beyond fp32's range) sets DION_STATUS_NONFINITE, and the coefficient is NaN. */
 int dion_grad_norm(dion_ctx* ctx, const dion_grad* list, int count, int norm_type, float max_norm, float* norm_out,
                    float* each_out, float* coef_out, void* cuda_stream);
 
@@ -359,7 +360,8 @@ typedef struct {
 
 /* One AdamW step on a list of parameters:  g = s G,  M <- beta1 M + (1 - beta1) g,  V <- beta2 V + (1 - beta2) g^2,
  * X <- (1 - lr wd) X - lr (M / (1 - beta1^t)) / (sqrt(V / (1 - beta2^t)) + eps), lr being lr * lr_scale.  The arithmetic is
- * fp32.  A NaN or Inf in G stays in its element. */
+ * fp32 (root and quotient within 2^-22).  A NaN or Inf in G stays in its element; with eps = 0 an element whose moments are both
+ * zero divides zero by zero. */
 int dion_adamw_step(dion_ctx* ctx, const dion_param* list, int count, const dion_rule* rule, float lr, void* cuda_stream);
 
 /* One Lion step:  g = s G,  X <- (1 - lr wd) X - lr sign(beta1 M + (1 - beta1) g),  M <- beta2 M + (1 - beta2) g, with

@@ -85,6 +85,7 @@ struct Clip {
   const float* coef;             // the coefficient on the device, or, where it is NULL,
   const float* norms;            // the norms of parts of the whole, of which it is made
   int count, inf;
+  int in_place;                  // every array of the launch
   float max_norm;
   float* norm_out;
   float* coef_out;
@@ -350,11 +351,13 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
     const Acc<INF> r = block_reduce(acc, red);
     if (threadIdx.x == 0) s->part[blockIdx.x] = r.kept();
   }
-  __threadfence();
-  if (threadIdx.x == 0) last = atomicAdd(&s->ticket, 1u) == gridDim.x - 1;
+  if (threadIdx.x == 0) {      // (it alone has written)
+    __threadfence();
+    last = atomicAdd(&s->ticket, 1u) == gridDim.x - 1;
+    __threadfence();
+  }
   __syncthreads();
   if (!last) return;
-  __threadfence();
   Acc<INF> all;
   if (each) {
     // Every partial result in one round trip.  Those of array i begin with the block that owns its first tile and end with the one
@@ -565,9 +568,6 @@ template <int CAP>
 __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __grid_constant__ Table<ScaleItem, CAP> t, const Clip c) {
   __shared__ double red[THREADS / 32];
   __shared__ float shared_coef;
-  // the last blocks of the list first: what the norm's launch read last is still in L2
-  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = t.tiles * b / G, t1 = t.tiles * (b + 1) / G;
-  i64 i = t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
   float coef;
   if (c.coef != nullptr) {
@@ -592,7 +592,10 @@ __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __
     __syncthreads();
     coef = shared_coef;
   }
-  for (i64 tile = t0; tile < t1; ++i) {
+  if (coef == 1.f && c.in_place) return;
+  // the last blocks of the list first: what the norm's launch read last is still in L2
+  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = t.tiles * b / G, t1 = t.tiles * (b + 1) / G;
+  for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
     const ScaleItem& it = t.item[i];
     i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
     if (end > t1) end = t1;

@@ -13,16 +13,17 @@ namespace list {
 
 namespace {
 
-// Blocks: one wave of resident ones (the kernels' launch bounds); of large lists more, each with a few tiles, since blocks that
-// start in order keep what is in flight close together in memory (AdamW on 268M parameters: 1249 us in one wave, 1123 with 4
-// tiles a block, 1156 with 2; scaling 872M bf16 elements with their norm: 993 in one wave, 876, 785 and 794 with 4, 8 and 16;
-// Lion 717, 650 with 4 at four resident blocks; the norm alone does not care: 505 and 504).
+// Blocks: one wave of resident ones (the kernels' launch bounds); of long lists more, each with a few tiles.  Blocks that start
+// in order keep what is in flight close together in memory, and an SM that is slower takes fewer (AdamW on 268M parameters:
+// 1249 us in one wave, 1238 with chunks dealt to one wave in turn, 1114 with 4 tiles a block, 1156 with 2; Lion 717, 647 with 4).
+// Scaling 872M bf16 elements with their norm: 993 in one wave, 788, 796, 799, 813 with 8, 16, 24, 32 tiles; but where the
+// coefficient is 1 every block is started for nothing: 1074M elements 307 us for the norm, 375, 342, 330, 325 with the launch behind it.
 struct Shape {
   int resident, tiles;      // blocks per SM of one wave, tiles per block beyond it
   i64 most;                 // blocks
 };
 constexpr i64 ANY = INT32_MAX;
-constexpr Shape NORM_SHAPE = {NORM_RESIDENT, INT32_MAX, MOST_NORM_BLOCKS}, SCALE_SHAPE = {SCALE_RESIDENT, 8, ANY},
+constexpr Shape NORM_SHAPE = {NORM_RESIDENT, INT32_MAX, MOST_NORM_BLOCKS}, SCALE_SHAPE = {SCALE_RESIDENT, 24, ANY},
                 ADAMW_SHAPE = {ADAMW_RESIDENT, 4, ANY}, LION_SHAPE = {LION_RESIDENT, 4, ANY};
 // Arrays in one launch: its parameters end at 32764 bytes.  Small lists take small parameters.
 constexpr int FEW = 24, SOME = 80;
@@ -294,6 +295,7 @@ int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
   do {
     t.tiles = 0;
     t.count = 0;
+    c.in_place = 1;
     while (done < count && t.count < CAP) {
       const dion_grad& a = list[done];
       ScaleItem* it = &t.item[t.count++];
@@ -301,6 +303,7 @@ int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
       take(list, count, true, &done, &rows, &cols);
       it->g = a.G; it->ldg = a.ldg;
       it->out = a.out; it->ldo = a.ldo;
+      c.in_place = c.in_place && a.G == a.out;
       const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}, {a.out, a.ldo, shift_of(a.out_dtype)}};
       it->w = plan(rows, cols, a.g_dtype, a.out_dtype, arrays, &t.tiles);
     }

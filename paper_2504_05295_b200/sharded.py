@@ -103,3 +103,39 @@ class ShardedStepper:
         all_reduce_sum(self.sumsq, self.group)
         for l, d in enumerate(self.descs):
             opt.shard_finish(d, nt, self.parts[l], self.W[l], self.sumsq[l], self.flags[l:l + 1], lr, stream)
+
+
+class ShardedClipper:
+    """Clips the gradients of a sharded model by their global norm.
+
+    shards: `binding.GradList` of what this rank alone holds (its column shards); whole: optional list of gradients that
+    every rank holds alike (norm gains, biases), which count once.  One all-gather of a number per rank; the norm of the
+    norms is taken in the library, in the order of the ranks, so every rank scales by the same bits.  `norm` and `coef`
+    (device floats) hold the last call's norm and coefficient, the latter for `grad_scale` of the steps on `whole`."""
+
+    def __init__(self, opt, shards, whole=None, device=None, group=None):
+        self.opt, self.shards, self.whole, self.group = opt, shards, whole, group
+        self.world = _world(group)
+        self.norms = torch.zeros(self.world + (whole is not None), dtype=torch.float32, device=device)
+        self.mine = torch.zeros(1, dtype=torch.float32, device=device)
+        self.norm = torch.zeros(1, dtype=torch.float32, device=device)
+        self.coef = torch.zeros(1, dtype=torch.float32, device=device)
+
+    def clip(self, max_norm: float, norm_type=2, scale_whole: bool = True,
+             stream: Optional[torch.cuda.Stream] = None) -> None:
+        """scale_whole=False leaves the gradients of `whole` to steps that take `coef`."""
+        if stream is not None and self.norms.is_cuda:
+            with torch.cuda.stream(stream):      # (the collective runs on the current stream)
+                self._clip(max_norm, norm_type, scale_whole, stream)
+        else:
+            self._clip(max_norm, norm_type, scale_whole, stream)
+
+    def _clip(self, max_norm, norm_type, scale_whole, stream) -> None:
+        opt, world = self.opt, self.world
+        opt.grad_norm(self.shards, norm_type, norm_out=self.mine, stream=stream)
+        all_gather_layers(self.norms[:world].view(world, 1), self.mine, self.group)
+        if self.whole is not None:
+            opt.grad_norm(self.whole, norm_type, norm_out=self.norms[world:], stream=stream)
+        opt.clip_grads(self.shards, max_norm, norms=self.norms, norm_type=norm_type, norm_out=self.norm, coef_out=self.coef, stream=stream)
+        if self.whole is not None and scale_whole:
+            opt.clip_grads(self.whole, max_norm, norms=self.norms, norm_type=norm_type, stream=stream)

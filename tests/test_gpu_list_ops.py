@@ -634,3 +634,76 @@ def test_binding_checks(opt):
     with pytest.raises(binding.DionError):
         opt.adamw_step(binding.param_list([]), 0.1, 0)
     assert opt.get_status() == (0, 0)
+
+
+# ---- together, as a training step uses them ----------------------------------------------------------------------
+
+def test_training_steps_of_a_small_model(opt):
+    # matrices by Dion, embedding and gains by AdamW, biases by Lion, all clipped by one norm: every state
+    # against float64, step by step from the states that the device holds
+    from oracle import dion_oracle as orc
+    r = lambda *shape: torch.randn(*shape, generator=gen(sum(shape)), device="cuda")  # noqa: E731
+    E, gain, bias = r(50, 48) * 0.5, torch.ones(64, device="cuda"), torch.zeros(64, device="cuda")
+    W1, W2 = r(64, 48) * 0.2, r(96, 64) * 0.2
+    leaves = {"E": E, "gain": gain, "bias": bias, "W1": W1, "W2": W2}
+    params = {k: t.clone().requires_grad_() for k, t in leaves.items()}
+    M = {k: torch.zeros_like(t) for k, t in leaves.items()}
+    V = {k: torch.zeros_like(leaves[k]) for k in ("E", "gain")}
+    E16 = torch.zeros_like(E, dtype=torch.bfloat16)
+    Q = {k: torch.linalg.qr(r(leaves[k].shape[1], 8))[0].contiguous() for k in ("W1", "W2")}
+    tokens = torch.arange(32, device="cuda") % 50
+    target = r(32, 96)
+    lr, mu = 0.01, 0.95
+    for t in range(1, 4):
+        h = torch.relu(params["E"][tokens] @ params["W1"].t()) * params["gain"] + params["bias"]
+        loss = ((h @ params["W2"].t() - target) ** 2).mean() * 10.0
+        grads = dict(zip(params, torch.autograd.grad(loss, list(params.values()))))
+        before = {k: p.detach().clone() for k, p in params.items()}
+        kept = {"M": {k: v.clone() for k, v in M.items()}, "V": {k: v.clone() for k, v in V.items()}, "G": {k: g.clone() for k, g in grads.items()},
+                "Q": {k: v.clone() for k, v in Q.items()}}
+        X = {k: p.data for k, p in params.items()}
+        matrices, others = binding.grad_list([grads["W1"], grads["W2"]]), binding.grad_list([grads[k] for k in ("E", "gain", "bias")])
+        norms, norm, coef = torch.zeros(2, device="cuda"), scalar(), scalar()
+        opt.grad_norm(matrices, norm_out=norms[:1])
+        opt.grad_norm(others, norm_out=norms[1:])
+        max_norm = 0.5 * norm64(list(kept["G"].values()))
+        opt.clip_grads(matrices, max_norm, norms=norms, norm_out=norm, coef_out=coef)
+        opt.step_grouped([(X[k], M[k], grads[k], Q[k]) for k in ("W1", "W2")], lr)
+        opt.adamw_step(binding.param_list([binding.param_desc(X["E"], grads["E"], M["E"], V["E"], E16, weight_decay=0.1),
+                                           binding.param_desc(X["gain"], grads["gain"], M["gain"], V["gain"])]), lr, t, grad_scale=coef)
+        opt.lion_step(binding.param_list([binding.param_desc(X["bias"], grads["bias"], M["bias"])]), lr, 0.9, 0.95, grad_scale=coef)
+        assert opt.get_status() == (0, 0)
+        s = 0.5
+        assert abs(float(norm) - 2 * max_norm) <= (NORM + 2 * u) * 2 * max_norm and abs(float(coef) - s) <= (COEF + 4 * u) * s
+        check_clipped([grads[k] for k in ("W1", "W2")], [grads[k] for k in ("W1", "W2")], [kept["G"][k] for k in ("W1", "W2")], s)
+        for k in ("W1", "W2"):
+            d = lambda x: x.double().cpu().numpy()  # noqa: E731
+            want = orc.step(d(before[k]), d(kept["M"][k]), d(kept["G"][k]) * s, d(kept["Q"][k]), mu, lr, 1e-8)
+            for name, got in (("X", X[k]), ("M", M[k]), ("Q", Q[k])):      # (the library's stated bound)
+                assert np.linalg.norm(d(got) - getattr(want, name)) <= 1e-4 * np.linalg.norm(getattr(want, name)), (t, k, name)
+        c = float(coef.double())
+        for k, decay in (("E", f32(0.1)), ("gain", 0.0)):
+            after = {"X": X[k], "G": grads[k], "M": M[k], "V": V[k]}
+            if k == "E":
+                after["X16"] = E16
+            check_step({"X": before[k], "G": kept["G"][k], "M": kept["M"][k], "V": kept["V"][k]}, after, True, f32(lr), 0.9, 0.95, 1e-8, t, c, 1.0, decay)
+        check_step({"X": before["bias"], "G": kept["G"]["bias"], "M": kept["M"]["bias"]}, {"X": X["bias"], "G": grads["bias"], "M": M["bias"]},
+                   False, f32(lr), 0.9, 0.95, 0.0, t, c, 1.0, 0.0)
+
+
+def test_sharded_clipper_on_one_rank(opt):
+    from paper_2504_05295_b200 import sharded
+    shards, whole = torch.randn((300, 77), generator=gen(1), device="cuda"), torch.randn(4096, generator=gen(2), device="cuda")
+    both = [shards.clone(), whole.clone()]
+    want = norm64(both)
+    clipper = sharded.ShardedClipper(opt, binding.grad_list([shards]), binding.grad_list([whole]), "cuda")
+    clipper.clip(1.0, scale_whole=False)
+    assert abs(float(clipper.norm) - want) <= (NORM + NORM) * want
+    check_clipped([shards], [shards], both[:1], float(clipper.coef.double()))
+    assert torch.equal(whole, both[1])
+    shards.copy_(both[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    clipper.clip(1.0, stream=side)
+    side.synchronize()
+    check_clipped([shards, whole], [shards, whole], both, float(clipper.coef.double()))
