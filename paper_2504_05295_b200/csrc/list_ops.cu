@@ -25,9 +25,10 @@ struct Shape {
 constexpr i64 ANY = INT32_MAX;
 constexpr Shape NORM_SHAPE = {NORM_RESIDENT, INT32_MAX, MOST_NORM_BLOCKS}, SCALE_SHAPE = {SCALE_RESIDENT, 24, ANY},
                 ADAMW_SHAPE = {ADAMW_RESIDENT, 4, ANY}, LION_SHAPE = {LION_RESIDENT, 4, ANY};
-// Arrays in one launch: its parameters end at 32764 bytes.  Small lists take small parameters.
-constexpr int FEW = 24, SOME = 80;
-constexpr int MANY_NORM = 500, MANY_SCALE = 400, MANY_STEP = 250;
+// Arrays in one launch: its parameters end at 32764 bytes.  A launch's parameters are copied whole (28 KB cost 3 us more than 7 KB), so
+// tables come in four sizes.
+constexpr int FEW = 24, SOME = 80, MORE = 180;
+constexpr int MANY_NORM = 500, MANY_SCALE = 400, MANY_STEP = 250, MANY_CLUSTER = CLUSTER_TILES;
 constexpr i64 MAX_ELEMENTS = (i64)1 << 50;      // (no element count or byte offset overflows)
 
 template <typename... KArgs, typename... Args>
@@ -336,7 +337,8 @@ bool cluster_launch(const Where& w, const dion_grad* list, int count, bool scale
 }
 bool cluster_launch(const Where& w, const dion_grad* list, int count, bool scale, bool inf, const NormOut& o, int* rc) {
   const int items = items_of(list, count, scale);
-  return items <= FEW ? cluster_launch<FEW>(w, list, count, scale, inf, o, rc) : items <= SOME && cluster_launch<SOME>(w, list, count, scale, inf, o, rc);
+  if (items > CLUSTER_TILES) return false;
+  return items <= FEW ? cluster_launch<FEW>(w, list, count, scale, inf, o, rc) : cluster_launch<MANY_CLUSTER>(w, list, count, scale, inf, o, rc);
 }
 
 template <int CAP, bool ADAMW>
@@ -370,8 +372,9 @@ int step_launches(const Where& w, const dion_param* list, int count, Rule r, flo
 template <bool ADAMW>
 int step(const Where& w, const dion_param* list, int count, const Rule& r, float lr) {
   const int items = items_of(list, count, ADAMW);
-  return items <= FEW ? step_launches<FEW, ADAMW>(w, list, count, r, lr) : items <= SOME ? step_launches<SOME, ADAMW>(w, list, count, r, lr)
-                      : step_launches<MANY_STEP, ADAMW>(w, list, count, r, lr);
+  if (items <= FEW) return step_launches<FEW, ADAMW>(w, list, count, r, lr);
+  if (items <= SOME) return step_launches<SOME, ADAMW>(w, list, count, r, lr);
+  return items <= MORE ? step_launches<MORE, ADAMW>(w, list, count, r, lr) : step_launches<MANY_STEP, ADAMW>(w, list, count, r, lr);
 }
 
 template <typename K>
@@ -386,13 +389,21 @@ bool load(K kernel) {
 size_t scratch_bytes() { return sizeof(Scratch); }
 static_assert(MANY_NORM <= MOST_PARTS - MOST_NORM_BLOCKS, "a launch's partial results fit");
 
+namespace {
+
+template <int CAP>
+bool load_tables() {
+  return load(k_list_norm<CAP, false>) && load(k_list_norm<CAP, true>) && load(k_list_scale<CAP>) && load(k_list_step<CAP, false>) &&
+         load(k_list_step<CAP, true>);
+}
+
+}  // namespace
+
 int configure() {
-  const bool ok = load(k_list_cluster<FEW, false>) && load(k_list_cluster<FEW, true>) && load(k_list_cluster<SOME, false>) && load(k_list_cluster<SOME, true>) &&
-                  load(k_list_norm<SOME, false>) && load(k_list_norm<SOME, true>) && load(k_list_scale<SOME>) && load(k_list_step<SOME, false>) &&
-                  load(k_list_step<SOME, true>) && load(k_list_norm<FEW, false>) && load(k_list_norm<FEW, true>) && load(k_list_norm<MANY_NORM, false>) &&
-                  load(k_list_norm<MANY_NORM, true>) && load(k_list_scale<FEW>) && load(k_list_scale<MANY_SCALE>) &&
-                  load(k_list_step<FEW, false>) && load(k_list_step<FEW, true>) && load(k_list_step<MANY_STEP, false>) &&
-                  load(k_list_step<MANY_STEP, true>);
+  const bool ok = load_tables<FEW>() && load_tables<SOME>() && load_tables<MORE>() && load(k_list_norm<MANY_NORM, false>) &&
+                  load(k_list_norm<MANY_NORM, true>) && load(k_list_scale<MANY_SCALE>) && load(k_list_step<MANY_STEP, false>) &&
+                  load(k_list_step<MANY_STEP, true>) && load(k_list_cluster<FEW, false>) && load(k_list_cluster<FEW, true>) &&
+                  load(k_list_cluster<MANY_CLUSTER, false>) && load(k_list_cluster<MANY_CLUSTER, true>);
   return ok ? DION_OK : DION_ERR_CUDA;
 }
 
@@ -502,8 +513,9 @@ NormOut norm_out_of(const Where& w, float max_norm, float* norm_out, float* coef
 
 int long_norm(const Where& w, const dion_grad* list, int count, bool inf, const NormOut& o, float* each_out) {
   const int items = each_out != nullptr ? count : items_of(list, count, false);
-  return items <= FEW ? norm_launches<FEW>(w, list, count, inf, o, each_out) : items <= SOME ? norm_launches<SOME>(w, list, count, inf, o, each_out)
-                      : norm_launches<MANY_NORM>(w, list, count, inf, o, each_out);
+  if (items <= FEW) return norm_launches<FEW>(w, list, count, inf, o, each_out);
+  if (items <= SOME) return norm_launches<SOME>(w, list, count, inf, o, each_out);
+  return items <= MORE ? norm_launches<MORE>(w, list, count, inf, o, each_out) : norm_launches<MANY_NORM>(w, list, count, inf, o, each_out);
 }
 
 }  // namespace
@@ -532,8 +544,9 @@ int clip_grads(const Where& w, const dion_grad* list, int count, float max_norm,
     c.coef = &((Scratch*)w.scratch)->coef;
   }
   const int items = items_of(list, count, true);
-  return items <= FEW ? scale_launches<FEW>(w, list, count, c) : items <= SOME ? scale_launches<SOME>(w, list, count, c)
-                      : scale_launches<MANY_SCALE>(w, list, count, c);
+  if (items <= FEW) return scale_launches<FEW>(w, list, count, c);
+  if (items <= SOME) return scale_launches<SOME>(w, list, count, c);
+  return items <= MORE ? scale_launches<MORE>(w, list, count, c) : scale_launches<MANY_SCALE>(w, list, count, c);
 }
 
 int param_step(const Where& w, bool adamw, const dion_param* list, int count, const dion_rule* rule, float lr) {

@@ -102,7 +102,7 @@ def test_norm_of_a_mixed_list(opt, kind):
     assert opt.get_status() == (0, 0)
 
 
-@pytest.mark.parametrize("count", [0, 1, 24, 25, 96, 97, 500, 501, 1234])
+@pytest.mark.parametrize("count", [0, 1, 24, 25, 80, 81, 96, 97, 180, 181, 500, 501, 1234])
 def test_norm_of_long_lists(opt, count):
     flat = torch.randn(count * 37 + 1, generator=gen(count), device="cuda")
     ts = [flat[37 * k:37 * k + 1 + k % 37] for k in range(count)]
@@ -316,7 +316,7 @@ def test_clip_by_given_norms(opt, kind):
     assert abs(float(norm2) - 2.0 * math.sqrt(1000)) <= NORM * float(norm2)
 
 
-@pytest.mark.parametrize("count", [25, 401, 1000])
+@pytest.mark.parametrize("count", [25, 81, 181, 401, 1000])
 def test_clip_long_lists(opt, count):
     flat = torch.randn(count * 41, generator=gen(count), device="cuda")
     before = flat.clone()
@@ -437,7 +437,7 @@ def test_step(opt, adamw, g, m, lies, copy):
 
 
 @pytest.mark.parametrize("adamw", [True, False], ids=["adamw", "lion"])
-@pytest.mark.parametrize("count", [0, 24, 25, 250, 251, 700])
+@pytest.mark.parametrize("count", [0, 24, 25, 81, 181, 250, 251, 700])
 def test_step_on_long_lists(opt, adamw, count):
     made = make_params([(1, 1 + k % 50) for k in range(count)], "bf16", "f32", [PLAIN], True, 7, adamw)
     before = [{k: t.clone() for k, t in ts.items()} for ts, _ in made]
