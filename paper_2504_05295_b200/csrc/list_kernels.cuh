@@ -57,7 +57,7 @@ struct StepItem {
 
 template <class Item, int CAP>
 struct Table {
-  i64 tiles;
+  i64 tiles, per, rem;           // tiles; block b takes `per` of them, and one more where b < rem
   int count;
   Item item[CAP];
 };
@@ -101,6 +101,15 @@ struct Rule {
   int first;                     // the first launch of a list: counts a cancelled step
   int* status;                   // [0] bits, [1] cancelled steps
 };
+
+// The first tile of block b, and the block that takes a tile.
+template <class Table>
+__device__ __forceinline__ i64 first_tile(const Table& t, i64 b) { return b * t.per + (b < t.rem ? b : t.rem); }
+template <class Table>
+__device__ __forceinline__ i64 owner_of(const Table& t, i64 tile) {
+  const i64 cut = t.rem * (t.per + 1);
+  return tile < cut ? row_of(tile, t.per + 1) : t.rem + row_of(tile - cut, t.per);
+}
 
 // The last array that starts at or before the tile.  Seven looks at a time: a look at the parameters is a round trip to memory
 // the first time, and these do not wait for one another.
@@ -328,7 +337,7 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
   __shared__ bool last;
   __shared__ double parts[MOST_PARTS];
   __shared__ int from[CAP], upto[CAP];
-  const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
+  const i64 G = gridDim.x, t0 = first_tile(t, blockIdx.x), t1 = first_tile(t, blockIdx.x + 1);
   i64 i = t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
   const bool each = o.each != nullptr;
@@ -365,8 +374,8 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
     for (int k = threadIdx.x; k < G + t.count; k += THREADS) parts[k] = __ldcg(&s->part[k]);
     for (int i = threadIdx.x; i < t.count; i += THREADS) {
       const i64 f = t.item[i].w.first, l = (i + 1 < t.count ? t.item[i + 1].w.first : t.tiles) - 1;
-      from[i] = f <= l ? (int)(((f + 1) * G - 1) / t.tiles) + i : 0;
-      upto[i] = f <= l ? (int)(((l + 1) * G - 1) / t.tiles) + i + 1 : 0;
+      from[i] = f <= l ? (int)owner_of(t, f) + i : 0;
+      upto[i] = f <= l ? (int)owner_of(t, l) + i + 1 : 0;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < t.count; i += THREADS) {
@@ -418,7 +427,7 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 1) k_list_cluster(const __gri
   const int rank = blockIdx.x, team = threadIdx.x / THREADS, lane = threadIdx.x % THREADS;
   asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (the others' shared memory is there once all have come)
   // tiles of this CTA, dealt to its teams in turn
-  const i64 t0 = t.tiles * rank / CLUSTER, t1 = t.tiles * (rank + 1) / CLUSTER;
+  const i64 t0 = first_tile(t, rank), t1 = first_tile(t, rank + 1);
   int item[KEPT];
 #pragma unroll
   for (int k = 0; k < KEPT; ++k) {
@@ -594,7 +603,7 @@ __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __
   }
   if (coef == 1.f && c.in_place) return;
   // the last blocks of the list first: what the norm's launch read last is still in L2
-  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = t.tiles * b / G, t1 = t.tiles * (b + 1) / G;
+  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = first_tile(t, b), t1 = first_tile(t, b + 1);
   for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
     const ScaleItem& it = t.item[i];
     i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
@@ -722,7 +731,7 @@ __device__ __forceinline__ void step_groups(const StepItem& it, const Part& p, c
 template <int CAP, bool ADAMW>
 __global__ void __launch_bounds__(THREADS, ADAMW ? ADAMW_RESIDENT : LION_RESIDENT) k_list_step(const __grid_constant__ Table<StepItem, CAP> t, const Rule r) {
   __shared__ float corr[2];
-  const i64 G = gridDim.x, t0 = t.tiles * blockIdx.x / G, t1 = t.tiles * (blockIdx.x + 1) / G;
+  const i64 G = gridDim.x, t0 = first_tile(t, blockIdx.x), t1 = first_tile(t, blockIdx.x + 1);
   i64 i = t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
   const float s = r.scale != nullptr ? *r.scale : 1.f;

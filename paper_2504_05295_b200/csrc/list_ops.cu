@@ -46,14 +46,15 @@ int launch_blocks(const Where& w, void (*kernel)(KArgs...), i64 blocks, int thre
   return DION_OK;
 }
 
-template <typename... KArgs, typename... Args>
-int launch(const Where& w, void (*kernel)(KArgs...), const Shape& shape, i64 tiles, const Args&... args) {
+template <class Table, typename... KArgs, typename... Args>
+int launch(const Where& w, void (*kernel)(KArgs...), const Shape& shape, Table& t, const Args&... args) {
   i64 blocks = (i64)w.sm_count * shape.resident;
-  if (tiles / shape.tiles > blocks) blocks = tiles / shape.tiles;
+  if (t.tiles / shape.tiles > blocks) blocks = t.tiles / shape.tiles;
   if (blocks > shape.most) blocks = shape.most;
-  if (blocks > tiles) blocks = tiles;
+  if (blocks > t.tiles) blocks = t.tiles;
   if (blocks < 1) blocks = 1;
-  return launch_blocks(w, kernel, blocks, THREADS, 1, args...);
+  t.per = t.tiles / blocks; t.rem = t.tiles % blocks;
+  return launch_blocks(w, kernel, blocks, THREADS, 1, t, args...);
 }
 
 inline int bytes_of(int dtype) { return dtype == DION_BF16 ? 2 : 4; }
@@ -283,8 +284,8 @@ int norm_launches(const Where& w, const dion_grad* list, int count, bool inf, No
       it->w = plan(rows, cols, a.g_dtype, DION_F32, arrays, &t.tiles);
     }
     o.last = done == count;
-    if (inf) LIST_TRY(launch(w, k_list_norm<CAP, true>, NORM_SHAPE, t.tiles, t, o));
-    else LIST_TRY(launch(w, k_list_norm<CAP, false>, NORM_SHAPE, t.tiles, t, o));
+    if (inf) LIST_TRY(launch(w, k_list_norm<CAP, true>, NORM_SHAPE, t, o));
+    else LIST_TRY(launch(w, k_list_norm<CAP, false>, NORM_SHAPE, t, o));
   } while (done < count);
   return DION_OK;
 }
@@ -308,7 +309,7 @@ int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
       const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}, {a.out, a.ldo, shift_of(a.out_dtype)}};
       it->w = plan(rows, cols, a.g_dtype, a.out_dtype, arrays, &t.tiles);
     }
-    LIST_TRY(launch(w, k_list_scale<CAP>, SCALE_SHAPE, t.tiles, t, c));
+    LIST_TRY(launch(w, k_list_scale<CAP>, SCALE_SHAPE, t, c));
     c.norm_out = nullptr; c.coef_out = nullptr;
   } while (done < count);
   return DION_OK;
@@ -331,6 +332,7 @@ bool cluster_launch(const Where& w, const dion_grad* list, int count, bool scale
     it->w = plan(rows, cols, a.g_dtype, a.out_dtype, arrays, &t.tiles);
     if (t.tiles > CLUSTER_TILES) return false;
   }
+  t.per = t.tiles / CLUSTER; t.rem = t.tiles % CLUSTER;
   *rc = inf ? launch_blocks(w, k_list_cluster<CAP, true>, CLUSTER, THREADS * TEAMS, CLUSTER, t, o, (int)scale)
             : launch_blocks(w, k_list_cluster<CAP, false>, CLUSTER, THREADS * TEAMS, CLUSTER, t, o, (int)scale);
   return true;
@@ -364,7 +366,7 @@ int step_launches(const Where& w, const dion_param* list, int count, Rule r, flo
       const Array arrays[] = {{it->X, a.ldx, 2}, {a.G, a.ldg, shift_of(a.g_dtype)}, {a.M, a.ldm, shift_of(a.m_dtype)}, {it->V, a.ldv, 2}, {it->X16, a.ldx16, 1}};
       it->w = plan(rows, cols, a.g_dtype, a.m_dtype, arrays, &t.tiles);
     }
-    LIST_TRY(launch(w, k_list_step<CAP, ADAMW>, ADAMW ? ADAMW_SHAPE : LION_SHAPE, t.tiles, t, r));
+    LIST_TRY(launch(w, k_list_step<CAP, ADAMW>, ADAMW ? ADAMW_SHAPE : LION_SHAPE, t, r));
   }
   return DION_OK;
 }
