@@ -2,9 +2,9 @@
 // steps of parameters that are not matrices.
 //
 // One launch covers a whole list.  The arrays' descriptors travel in the launch's parameters (no table in device memory: nothing
-// to copy before the launch, and a captured launch keeps its own).  The list is cut into tiles, numbered through; block b of G
-// walks the tiles [T b / G, T (b + 1) / G), so every block has the same share whatever the arrays' sizes, finds its first array by
-// one search and steps from array to array after that.
+// to copy before the launch, and a captured launch keeps its own).  The list is cut into tiles, numbered through; every block
+// takes the same number of neighbouring tiles (or one more), whatever the arrays' sizes, finds its first array by one search and
+// steps from array to array after that.
 #pragma once
 
 #include "dion_common.cuh"
@@ -208,7 +208,7 @@ __device__ __forceinline__ i64 row_at(const Walk& w, i64 u) { return w.per_row =
 __device__ __forceinline__ Spot group_at(const Walk& w, i64 u) {
   Spot s;
   s.row = row_at(w, u);
-  s.col = (u - s.row * w.per_row) * W - ((w.phase + (int)s.row * w.shift) & (W - 1));
+  s.col = (u - s.row * w.per_row) * W - ((w.phase + (uint32_t)s.row * w.shift) & (W - 1));
   s.lo = s.col < 0 ? (int)-s.col : 0;
   s.hi = w.width - s.col < W ? (int)(w.width - s.col) : W;      // (below lo: a place that this row does not fill)
   return s;

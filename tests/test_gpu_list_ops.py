@@ -636,6 +636,83 @@ def test_binding_checks(opt):
     assert opt.get_status() == (0, 0)
 
 
+# ---- calls at the edges of what the documentation allows ---------------------------------------------------------
+
+def test_slices_of_one_matrix_in_one_call(opt):
+    # columns, and every other row, of one matrix as entries of one list: each element is scaled once
+    for cut in (lambda t: [t[:, :100], t[:, 100:133], t[:, 133:]], lambda t: [t[0::2], t[1::2]], lambda t: [t[:50], t[50:51], t[51:]]):
+        t = torch.randn((97, 300), generator=gen(1), device="cuda")
+        before, parts = t.clone(), None
+        parts = cut(t)
+        opt.clip_grads(binding.grad_list(parts), 0.5 * norm64([before]))
+        check_clipped([t], [t], [before], 0.5)
+        X, M, V = torch.randn((97, 300), generator=gen(2), device="cuda"), torch.zeros(97, 300, device="cuda"), torch.zeros(97, 300, device="cuda")
+        old = dict(X=X.clone(), G=t.clone(), M=M.clone(), V=V.clone())
+        opt.adamw_step(binding.param_list([binding.param_desc(*p) for p in zip(cut(X), cut(t), cut(M), cut(V))]), 0.01, 1)
+        check_step(old, dict(X=X, G=t, M=M, V=V), True, f32(0.01), 0.9, 0.95, 1e-8, 1, 1.0, 1.0, 0.0)
+
+
+def test_one_gradient_into_two_results(opt):
+    for n in (1000, 700000):
+        g = torch.randn(n, generator=gen(1), device="cuda")
+        before = g.clone()
+        outs = [torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")]
+        opt.clip_grads(binding.grad_list([g, g], outs), 0.1)
+        check_clipped([g, g], outs, [before, before], 0.1 / (math.sqrt(2) * norm64([before])))
+        assert torch.equal(g, before)
+
+
+def test_shapes_of_any_rank(opt):
+    ts = [torch.randn(s, generator=gen(k), device="cuda") for k, s in enumerate([(), (3,), (2, 3, 5), (1, 1, 1, 7), (4, 0, 2), (64, 3, 3, 3)])]
+    out, each = scalar(), torch.full((len(ts),), -1.0, device="cuda")
+    opt.grad_norm(binding.grad_list(ts), norm_out=out, each_out=each)
+    assert abs(float(out) - norm64(ts)) <= NORM * norm64(ts)
+    assert all(abs(e - norm64([t])) <= NORM * norm64([t]) for e, t in zip(each.tolist(), ts))
+    M = [torch.zeros_like(t) for t in ts]
+    X = [torch.zeros_like(t) for t in ts]
+    opt.lion_step(binding.param_list([binding.param_desc(x, g, m) for x, g, m in zip(X, ts, M)]), 0.5)
+    assert all(torch.equal(x, -0.5 * torch.sign(t)) for x, t in zip(X, ts))
+
+
+def test_two_contexts_at_once(opt):
+    # one context per stream; long lists, so that the launches overlap
+    streams, ts, outs = [torch.cuda.Stream() for _ in range(2)], [], []
+    with binding.Dion() as other:
+        for k in range(2):
+            ts.append(torch.randn(30000000 + 12345 * k, generator=gen(k), device="cuda"))
+            outs.append((scalar(), scalar(), torch.zeros(1, device="cuda")))
+        want = [norm64([t]) for t in ts]
+        torch.cuda.synchronize()
+        for rep in range(20):
+            for o, st, t, (norm, inf, each) in zip((opt, other), streams, ts, outs):
+                items = binding.grad_list([t])
+                o.grad_norm(items, norm_out=norm, each_out=each, stream=st)
+                o.clip_grads(items, 1e9, norm_type="inf", norm_out=inf, stream=st)
+        torch.cuda.synchronize()
+        for t, w, (norm, inf, each) in zip(ts, want, outs):
+            assert abs(float(norm) - w) <= NORM * w and torch.equal(norm, each) and float(inf) == norm64([t], "inf")
+        assert opt.get_status() == other.get_status() == (0, 0)
+
+
+def test_graphs_that_share_a_context(opt):
+    # two graphs of one context, replayed in turn on one stream: neither leaves anything that the other trips over
+    ts = [torch.randn(n, generator=gen(n), device="cuda") for n in (5000000, 3000)]
+    outs = [scalar() for _ in ts]
+    graphs = []
+    for t, out in zip(ts, outs):
+        items, each = binding.grad_list([t[:1000], t[1001:]]), torch.zeros(2, device="cuda")
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            opt.grad_norm(items, norm_out=out, each_out=each)
+        graphs.append((g, norm64([t[:1000], t[1001:]]), out, each, items))
+    eager = scalar()
+    for _ in range(5):
+        for g, want, out, each, items in graphs:
+            g.replay()
+            opt.grad_norm(items, norm_out=eager, each_out=each)
+            assert abs(float(out) - want) <= NORM * want and torch.equal(out, eager)
+
+
 # ---- together, as a training step uses them ----------------------------------------------------------------------
 
 def test_training_steps_of_a_small_model(opt):
