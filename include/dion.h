@@ -292,7 +292,9 @@ int dion_shard_finish(dion_ctx* ctx, const dion_matrix* a, int64_t n_total, cons
  * Nothing that a call writes may be touched twice by it: neither the same array twice in a list nor overlapping ones
  * (DION_ERR_ALIAS); column slices of one matrix do not overlap.  dion_grad_norm takes an array twice and counts it twice.
  * The calls are asynchronous on `cuda_stream`, allocate nothing, leave the calling thread's current device as it was and may
- * be captured into a CUDA graph (the host values of the call, lr and step among them, are those of the capture).
+ * be captured into a CUDA graph (the host values of the call, lr and step among them, are those of the capture).  A captured
+ * call has scratch of its own, so graphs of one context may run side by side (the last 63 captured calls over lists, that is:
+ * beyond these they take the same scratch again in turn); direct calls on one context must not overlap, as everywhere.
  * Results do not depend on timing: the same call gives the same bits. */
 typedef enum { DION_NORM_2 = 0, DION_NORM_INF = 1 } dion_norm;
 

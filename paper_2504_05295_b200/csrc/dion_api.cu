@@ -26,6 +26,7 @@ namespace {
 constexpr int MAX_GRAPHS = 64;             // cached step graphs per context (least recently used goes first)
 constexpr i64 GRAPH_MAX_ELEMS = (i64)2048 * 2048;   // graph replay for matrices up to this many elements (launch-bound steps)
 constexpr int MAX_FLAG_SLOTS = 4096;      // step slots of OS_SLOT_INTS ints each; the last MAX_GRAPHS belong to the cached graphs
+constexpr int LIST_SLOTS = 64;             // scratch slots of the calls over lists: the first for direct calls, the others for captured ones in turn
 constexpr int MAX_CHAIN = 64;              // matrices of one shape stepped together by dion_step_grouped
 constexpr size_t GROUP_SCRATCH_BYTES = (size_t)16 << 30;  // scratch dion_step_grouped may use for that (or cfg.workspace_bytes)
 constexpr int MAX_ROUNDS = 6;             // adaptive Cholesky QR rounds
@@ -112,7 +113,8 @@ struct dion_ctx {
   int flag_cursor;
   int* flow_ctl = nullptr;   // progress counters of k_chol_flow (zero between launches)
   i64 flow_ctl_cap = 0;
-  void* list_scratch = nullptr;   // partial sums of the calls over lists
+  char* list_scratch = nullptr;   // partial sums of the calls over lists: LIST_SLOTS slots
+  int list_cursor = 0;
   int64_t launches;
   // per-phase profiling (off by default)
   bool prof_on;
@@ -2587,7 +2589,7 @@ int dion_init(dion_ctx** out, const dion_config* cfg) {
   c->sm_count = prop.multiProcessorCount;
   void* p = nullptr;
   constexpr size_t ctl_bytes = (sizeof(int) * (8 + MAX_FLAG_SLOTS * OS_SLOT_INTS + 24 + FLOW_CTL_INTS) + 127) / 128 * 128;
-  const size_t int_bytes = ctl_bytes + list::scratch_bytes();
+  const size_t int_bytes = ctl_bytes + LIST_SLOTS * list::scratch_bytes();
   if (cudaMalloc(&p, int_bytes) != cudaSuccess) { delete c; return DION_ERR_NOMEM; }
   c->dev_ints = (int*)p;
   c->flow_ctl = c->dev_ints + 8 + MAX_FLAG_SLOTS * OS_SLOT_INTS + 24;      // (128-byte aligned)
@@ -2960,8 +2962,21 @@ struct OnDevice {
   ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
 };
 
+// A captured call keeps a slot of its own, so graphs share no scratch with one another or with direct calls.
+void* list_slot(void* owner, cudaStream_t st) {
+  dion_ctx* c = (dion_ctx*)owner;
+  int slot = 0;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(st, &capture) != cudaSuccess) cudaGetLastError();
+  if (capture == cudaStreamCaptureStatusActive) {
+    slot = 1 + c->list_cursor;
+    c->list_cursor = (c->list_cursor + 1) % (LIST_SLOTS - 1);
+  }
+  return c->list_scratch + slot * list::scratch_bytes();
+}
+
 list::Where list_call(dion_ctx* c, void* cuda_stream) {
-  return {c->sm_count, c->list_scratch, c->dev_ints, &c->launches, (cudaStream_t)cuda_stream};
+  return {c->sm_count, list_slot, c, c->dev_ints, &c->launches, (cudaStream_t)cuda_stream};
 }
 
 }  // namespace

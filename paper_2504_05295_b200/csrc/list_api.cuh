@@ -9,7 +9,8 @@ namespace list {
 // What a call needs of its context.
 struct Where {
   int sm_count;
-  void* scratch;          // scratch_bytes(), zero at first
+  void* (*scratch)(void* owner, cudaStream_t stream);      // scratch_bytes() for one call, zero at first; only long norms ask for it
+  void* owner;
   int* status;            // [0] status bits, [1] cancelled steps
   int64_t* launches;
   cudaStream_t stream;

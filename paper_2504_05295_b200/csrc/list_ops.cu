@@ -4,6 +4,7 @@
 #include <string.h>
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "list_api.cuh"
 #include "list_kernels.cuh"
@@ -31,8 +32,10 @@ constexpr int FEW = 24, SOME = 80, MORE = 180;
 constexpr int MANY_NORM = 500, MANY_SCALE = 400, MANY_STEP = 250, MANY_CLUSTER = CLUSTER_TILES;
 constexpr i64 MAX_ELEMENTS = (i64)1 << 50;      // (no element count or byte offset overflows)
 
+// (The arguments by address: a typed launch would copy the table once more.)
 template <typename... KArgs, typename... Args>
 int launch_blocks(const Where& w, void (*kernel)(KArgs...), i64 blocks, int threads, int cluster, const Args&... args) {
+  static_assert(sizeof...(KArgs) == sizeof...(Args) && (std::is_same<std::remove_cv_t<KArgs>, Args>::value && ...), "the kernel's own types");
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(threads); cfg.stream = w.stream;
   cudaLaunchAttribute attr[2];
@@ -42,7 +45,8 @@ int launch_blocks(const Where& w, void (*kernel)(KArgs...), i64 blocks, int thre
   attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
   ++*w.launches;
-  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) { cudaGetLastError(); return DION_ERR_CUDA; }
+  void* pointers[] = {const_cast<void*>((const void*)&args)...};
+  if (cudaLaunchKernelExC(&cfg, (const void*)kernel, pointers) != cudaSuccess) { cudaGetLastError(); return DION_ERR_CUDA; }
   return DION_OK;
 }
 
@@ -247,12 +251,6 @@ bool continues(const dion_param& a, const dion_param& b, bool v) {
          (a.X16 == nullptr ? b.X16 == nullptr : follows(a.X16, b.X16, n, 2)) && a.lr_scale == b.lr_scale && a.weight_decay == b.weight_decay &&
          dense(a, v) && dense(b, v);
 }
-template <class D>
-int items_of(const D* list, int count, bool more) {
-  int n = count > 0;
-  for (int i = 1; i < count; ++i) n += !continues(list[i - 1], list[i], more);
-  return n;
-}
 // The array at list[*at] with all that continue it, as one; *at is then behind them.
 template <class D>
 void take(const D* list, int count, bool more, int* at, i64* rows, i64* cols) {
@@ -265,51 +263,74 @@ void take(const D* list, int count, bool more, int* at, i64* rows, i64* cols) {
   *at = i + 1;
 }
 
-template <int CAP>
+// Calls f on the smallest table that holds the items of a filled one.
+template <int CAP, class Item, int BIG>
+void shrink(const Table<Item, BIG>& from, Table<Item, CAP>* to) {
+  to->tiles = from.tiles;
+  to->count = from.count;
+  std::copy(from.item, from.item + from.count, to->item);
+}
+template <class Item, int BIG, class F>
+int by_count(Table<Item, BIG>& t, const F& f) {
+  if (t.count <= FEW) { Table<Item, FEW> s; shrink(t, &s); return f(s); }
+  if (t.count <= SOME) { Table<Item, SOME> s; shrink(t, &s); return f(s); }
+  if (t.count <= MORE) { Table<Item, MORE> s; shrink(t, &s); return f(s); }
+  return f(t);
+}
+
+void put(const dion_grad* list, int count, bool apart, int* done, Table<NormItem, MANY_NORM>* t) {
+  const dion_grad& a = list[*done];
+  NormItem* it = &t->item[t->count++];
+  i64 rows = a.rows, cols = a.cols;
+  if (apart) ++*done; else take(list, count, false, done, &rows, &cols);
+  it->g = a.G; it->ldg = a.ldg;
+  const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}};
+  it->w = plan(rows, cols, a.g_dtype, DION_F32, arrays, &t->tiles);
+}
+
 int norm_launches(const Where& w, const dion_grad* list, int count, bool inf, NormOut o, float* each) {
-  Table<NormItem, CAP> t;
+  Table<NormItem, MANY_NORM> t;
   int done = 0;
   do {
     t.tiles = 0;
     t.count = 0;
     o.each = each != nullptr ? each + done : nullptr;
     o.use_carry = done > 0;
-    while (done < count && t.count < CAP) {
-      const dion_grad& a = list[done];
-      NormItem* it = &t.item[t.count++];
-      i64 rows = a.rows, cols = a.cols;
-      if (each != nullptr) ++done; else take(list, count, false, &done, &rows, &cols);
-      it->g = a.G; it->ldg = a.ldg;
-      const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}};
-      it->w = plan(rows, cols, a.g_dtype, DION_F32, arrays, &t.tiles);
-    }
+    while (done < count && t.count < MANY_NORM) put(list, count, each != nullptr, &done, &t);
     o.last = done == count;
-    if (inf) LIST_TRY(launch(w, k_list_norm<CAP, true>, NORM_SHAPE, t, o));
-    else LIST_TRY(launch(w, k_list_norm<CAP, false>, NORM_SHAPE, t, o));
+    LIST_TRY(by_count(t, [&](auto& table) {
+      constexpr int CAP = sizeof(table.item) / sizeof(NormItem);
+      return inf ? launch(w, k_list_norm<CAP, true>, NORM_SHAPE, table, o) : launch(w, k_list_norm<CAP, false>, NORM_SHAPE, table, o);
+    }));
   } while (done < count);
   return DION_OK;
 }
 
+// `scale` false: the norm alone is wanted, `out` is not looked at.
 template <int CAP>
+void put(const dion_grad* list, int count, bool scale, int* done, Table<ScaleItem, CAP>* t) {
+  const dion_grad& a = list[*done];
+  ScaleItem* it = &t->item[t->count++];
+  i64 rows, cols;
+  take(list, count, scale, done, &rows, &cols);
+  it->g = a.G; it->ldg = a.ldg;
+  it->out = a.out; it->ldo = a.ldo;
+  const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}, {scale ? a.out : nullptr, a.ldo, shift_of(a.out_dtype)}};
+  it->w = plan(rows, cols, a.g_dtype, a.out_dtype, arrays, &t->tiles);
+}
+
 int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
-  Table<ScaleItem, CAP> t;
+  Table<ScaleItem, MANY_SCALE> t;
   int done = 0;
   do {
     t.tiles = 0;
     t.count = 0;
     c.in_place = 1;
-    while (done < count && t.count < CAP) {
-      const dion_grad& a = list[done];
-      ScaleItem* it = &t.item[t.count++];
-      i64 rows, cols;
-      take(list, count, true, &done, &rows, &cols);
-      it->g = a.G; it->ldg = a.ldg;
-      it->out = a.out; it->ldo = a.ldo;
-      c.in_place = c.in_place && a.G == a.out;
-      const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}, {a.out, a.ldo, shift_of(a.out_dtype)}};
-      it->w = plan(rows, cols, a.g_dtype, a.out_dtype, arrays, &t.tiles);
+    while (done < count && t.count < MANY_SCALE) {
+      c.in_place = c.in_place && list[done].G == list[done].out;
+      put(list, count, true, &done, &t);
     }
-    LIST_TRY(launch(w, k_list_scale<CAP>, SCALE_SHAPE, t, c));
+    LIST_TRY(by_count(t, [&](auto& table) { return launch(w, k_list_scale<sizeof(table.item) / sizeof(ScaleItem)>, SCALE_SHAPE, table, c); }));
     c.norm_out = nullptr; c.coef_out = nullptr;
   } while (done < count);
   return DION_OK;
@@ -317,41 +338,39 @@ int scale_launches(const Where& w, const dion_grad* list, int count, Clip c) {
 
 // A short list in one launch (k_list_cluster).  false: it is too long.
 template <int CAP>
-bool cluster_launch(const Where& w, const dion_grad* list, int count, bool scale, bool inf, const NormOut& o, int* rc) {
-  Table<ScaleItem, CAP> t;
+int cluster_launch(const Where& w, Table<ScaleItem, CAP>& t, bool scale, bool inf, const NormOut& o) {
+  t.per = t.tiles / CLUSTER; t.rem = t.tiles % CLUSTER;
+  return inf ? launch_blocks(w, k_list_cluster<CAP, true>, CLUSTER, THREADS * TEAMS, CLUSTER, t, o, (int)scale)
+             : launch_blocks(w, k_list_cluster<CAP, false>, CLUSTER, THREADS * TEAMS, CLUSTER, t, o, (int)scale);
+}
+bool one_launch(const Where& w, const dion_grad* list, int count, bool scale, bool inf, const NormOut& o, int* rc) {
+  Table<ScaleItem, MANY_CLUSTER> t;
   t.tiles = 0;
   t.count = 0;
   for (int done = 0; done < count;) {
-    const dion_grad& a = list[done];
-    ScaleItem* it = &t.item[t.count++];
-    i64 rows, cols;
-    take(list, count, scale, &done, &rows, &cols);
-    it->g = a.G; it->ldg = a.ldg;
-    it->out = a.out; it->ldo = a.ldo;
-    const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}, {scale ? a.out : nullptr, a.ldo, shift_of(a.out_dtype)}};
-    it->w = plan(rows, cols, a.g_dtype, a.out_dtype, arrays, &t.tiles);
+    if (t.count == MANY_CLUSTER) return false;
+    put(list, count, scale, &done, &t);
     if (t.tiles > CLUSTER_TILES) return false;
   }
-  t.per = t.tiles / CLUSTER; t.rem = t.tiles % CLUSTER;
-  *rc = inf ? launch_blocks(w, k_list_cluster<CAP, true>, CLUSTER, THREADS * TEAMS, CLUSTER, t, o, (int)scale)
-            : launch_blocks(w, k_list_cluster<CAP, false>, CLUSTER, THREADS * TEAMS, CLUSTER, t, o, (int)scale);
+  if (t.count <= FEW) {
+    Table<ScaleItem, FEW> s;
+    shrink(t, &s);
+    *rc = cluster_launch(w, s, scale, inf, o);
+  } else {
+    *rc = cluster_launch(w, t, scale, inf, o);
+  }
   return true;
 }
-bool cluster_launch(const Where& w, const dion_grad* list, int count, bool scale, bool inf, const NormOut& o, int* rc) {
-  const int items = items_of(list, count, scale);
-  if (items > CLUSTER_TILES) return false;
-  return items <= FEW ? cluster_launch<FEW>(w, list, count, scale, inf, o, rc) : cluster_launch<MANY_CLUSTER>(w, list, count, scale, inf, o, rc);
-}
 
-template <int CAP, bool ADAMW>
-int step_launches(const Where& w, const dion_param* list, int count, Rule r, float lr) {
-  Table<StepItem, CAP> t;
+template <bool ADAMW>
+int step(const Where& w, const dion_param* list, int count, Rule r, float lr) {
+  Table<StepItem, MANY_STEP> t;
   int done = 0;
   while (done < count) {
     t.tiles = 0;
     t.count = 0;
     r.first = done == 0;
-    while (done < count && t.count < CAP) {
+    while (done < count && t.count < MANY_STEP) {
       const dion_param& a = list[done];
       StepItem* it = &t.item[t.count++];
       i64 rows, cols;
@@ -366,17 +385,12 @@ int step_launches(const Where& w, const dion_param* list, int count, Rule r, flo
       const Array arrays[] = {{it->X, a.ldx, 2}, {a.G, a.ldg, shift_of(a.g_dtype)}, {a.M, a.ldm, shift_of(a.m_dtype)}, {it->V, a.ldv, 2}, {it->X16, a.ldx16, 1}};
       it->w = plan(rows, cols, a.g_dtype, a.m_dtype, arrays, &t.tiles);
     }
-    LIST_TRY(launch(w, k_list_step<CAP, ADAMW>, ADAMW ? ADAMW_SHAPE : LION_SHAPE, t, r));
+    LIST_TRY(by_count(t, [&](auto& table) {
+      constexpr int CAP = sizeof(table.item) / sizeof(StepItem);
+      return launch(w, k_list_step<CAP, ADAMW>, ADAMW ? ADAMW_SHAPE : LION_SHAPE, table, r);
+    }));
   }
   return DION_OK;
-}
-
-template <bool ADAMW>
-int step(const Where& w, const dion_param* list, int count, const Rule& r, float lr) {
-  const int items = items_of(list, count, ADAMW);
-  if (items <= FEW) return step_launches<FEW, ADAMW>(w, list, count, r, lr);
-  if (items <= SOME) return step_launches<SOME, ADAMW>(w, list, count, r, lr);
-  return items <= MORE ? step_launches<MORE, ADAMW>(w, list, count, r, lr) : step_launches<MANY_STEP, ADAMW>(w, list, count, r, lr);
 }
 
 template <typename K>
@@ -388,7 +402,7 @@ bool load(K kernel) {
 
 }  // namespace
 
-size_t scratch_bytes() { return sizeof(Scratch); }
+size_t scratch_bytes() { return (sizeof(Scratch) + 127) / 128 * 128; }
 static_assert(MANY_NORM <= MOST_PARTS - MOST_NORM_BLOCKS, "a launch's partial results fit");
 
 namespace {
@@ -507,27 +521,24 @@ namespace {
 
 NormOut norm_out_of(const Where& w, float max_norm, float* norm_out, float* coef_out) {
   NormOut o = {};
-  o.scratch = (Scratch*)w.scratch;
   o.norm = norm_out; o.coef = coef_out; o.max_norm = max_norm;
   o.status = w.status;
   return o;
 }
 
-int long_norm(const Where& w, const dion_grad* list, int count, bool inf, const NormOut& o, float* each_out) {
-  const int items = each_out != nullptr ? count : items_of(list, count, false);
-  if (items <= FEW) return norm_launches<FEW>(w, list, count, inf, o, each_out);
-  if (items <= SOME) return norm_launches<SOME>(w, list, count, inf, o, each_out);
-  return items <= MORE ? norm_launches<MORE>(w, list, count, inf, o, each_out) : norm_launches<MANY_NORM>(w, list, count, inf, o, each_out);
+int long_norm(const Where& w, const dion_grad* list, int count, bool inf, NormOut& o, float* each_out) {
+  o.scratch = (Scratch*)w.scratch(w.owner, w.stream);
+  return norm_launches(w, list, count, inf, o, each_out);
 }
 
 }  // namespace
 
 int grad_norm(const Where& w, const dion_grad* list, int count, int norm_type, float max_norm, float* norm_out, float* each_out,
               float* coef_out) {
-  const NormOut o = norm_out_of(w, max_norm, norm_out, coef_out);
+  NormOut o = norm_out_of(w, max_norm, norm_out, coef_out);
   const bool inf = norm_type == DION_NORM_INF;
   int rc;
-  if (each_out == nullptr && cluster_launch(w, list, count, false, inf, o, &rc)) return rc;
+  if (each_out == nullptr && one_launch(w, list, count, false, inf, o, &rc)) return rc;
   return long_norm(w, list, count, inf, o, each_out);
 }
 
@@ -539,16 +550,13 @@ int clip_grads(const Where& w, const dion_grad* list, int count, float max_norm,
   if (norms != nullptr) {
     c.norms = norms; c.count = num_norms; c.norm_out = norm_out; c.coef_out = coef_out;
   } else {
-    const NormOut o = norm_out_of(w, max_norm, norm_out, coef_out);
+    NormOut o = norm_out_of(w, max_norm, norm_out, coef_out);
     int rc;
-    if (cluster_launch(w, list, count, true, c.inf, o, &rc)) return rc;
+    if (one_launch(w, list, count, true, c.inf, o, &rc)) return rc;
     LIST_TRY(long_norm(w, list, count, c.inf, o, nullptr));
-    c.coef = &((Scratch*)w.scratch)->coef;
+    c.coef = &o.scratch->coef;
   }
-  const int items = items_of(list, count, true);
-  if (items <= FEW) return scale_launches<FEW>(w, list, count, c);
-  if (items <= SOME) return scale_launches<SOME>(w, list, count, c);
-  return items <= MORE ? scale_launches<MORE>(w, list, count, c) : scale_launches<MANY_SCALE>(w, list, count, c);
+  return scale_launches(w, list, count, c);
 }
 
 int param_step(const Where& w, bool adamw, const dion_param* list, int count, const dion_rule* rule, float lr) {

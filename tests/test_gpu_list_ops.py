@@ -695,8 +695,8 @@ def test_two_contexts_at_once(opt):
 
 
 def test_graphs_that_share_a_context(opt):
-    # two graphs of one context, replayed in turn on one stream: neither leaves anything that the other trips over
-    ts = [torch.randn(n, generator=gen(n), device="cuda") for n in (5000000, 3000)]
+    # two graphs of one context, replayed in turn: neither leaves anything that the other trips over
+    ts = [torch.randn(n, generator=gen(n), device="cuda") for n in (5000000, 4000000)]
     outs = [scalar() for _ in ts]
     graphs = []
     for t, out in zip(ts, outs):
@@ -705,6 +705,19 @@ def test_graphs_that_share_a_context(opt):
         with torch.cuda.graph(g):
             opt.grad_norm(items, norm_out=out, each_out=each)
         graphs.append((g, norm64([t[:1000], t[1001:]]), out, each, items))
+    # ... and replayed side by side on two streams, with direct calls beside them
+    streams = [torch.cuda.Stream() for _ in graphs]
+    torch.cuda.synchronize()
+    direct = scalar()
+    for _ in range(200):
+        for st, (g, want, out, each, items) in zip(streams, graphs):
+            with torch.cuda.stream(st):
+                g.replay()
+        opt.grad_norm(binding.grad_list([ts[0]]), norm_out=direct)
+    torch.cuda.synchronize()
+    for g, want, out, each, items in graphs:
+        assert abs(float(out) - want) <= NORM * want and abs(float(each.double().square().sum().sqrt()) - want) <= 2 * NORM * want
+    assert abs(float(direct) - norm64([ts[0]])) <= NORM * float(direct)
     eager = scalar()
     for _ in range(5):
         for g, want, out, each, items in graphs:
