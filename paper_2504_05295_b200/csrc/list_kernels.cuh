@@ -572,44 +572,49 @@ __device__ __forceinline__ void scale_singles(const ScaleItem& it, const Part& p
   }
 }
 
+// The norm of given norms, in every lane of every warp.
+template <bool INF>
+__device__ __forceinline__ float norm_of_norms(const Clip& c) {
+  Acc<INF> a;
+  for (int k = threadIdx.x & 31; k < c.count; k += 32) a.add(c.norms[k]);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    if (INF) a.m = max(a.m, __shfl_xor_sync(0xffffffffu, a.m, d));
+    else a.s += __shfl_xor_sync(0xffffffffu, a.s, d);
+  }
+  return a.norm();
+}
+
 // out = coefficient * G.  Where G itself would be multiplied by one nothing is read or written.
 template <int CAP>
 __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __grid_constant__ Table<ScaleItem, CAP> t, const Clip c) {
-  __shared__ double red[THREADS / 32];
-  __shared__ float shared_coef;
+  // the last blocks of the list first: what the norm's launch read last is still in L2
+  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = first_tile(t, b), t1 = first_tile(t, b + 1);
+  // (The search and, further down, the first loads do not wait for the coefficient, except where it may say that nothing is to be done.)
+  i64 i = !c.in_place && t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
   float coef;
   if (c.coef != nullptr) {
     coef = *c.coef;
   } else {
-    Acc<false> sum;
-    Acc<true> top;
-    for (int k = threadIdx.x; k < c.count; k += THREADS) {
-      const float x = c.norms[k];
-      if (c.inf) top.add(x); else sum.add(x);
+    const float norm = c.inf ? norm_of_norms<true>(c) : norm_of_norms<false>(c);
+    coef = clip_coef(norm, c.max_norm);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      if (!isfinite(norm)) atomicOr(c.status, DION_STATUS_NONFINITE);
+      if (c.norm_out != nullptr) *c.norm_out = norm;
+      if (c.coef_out != nullptr) *c.coef_out = coef;
     }
-    float norm;
-    if (c.inf) norm = block_reduce(top, red).norm(); else norm = block_reduce(sum, red).norm();
-    if (threadIdx.x == 0) {
-      shared_coef = clip_coef(norm, c.max_norm);
-      if (blockIdx.x == 0) {
-        if (!isfinite(norm)) atomicOr(c.status, DION_STATUS_NONFINITE);
-        if (c.norm_out != nullptr) *c.norm_out = norm;
-        if (c.coef_out != nullptr) *c.coef_out = shared_coef;
-      }
-    }
-    __syncthreads();
-    coef = shared_coef;
   }
-  if (coef == 1.f && c.in_place) return;
-  // the last blocks of the list first: what the norm's launch read last is still in L2
-  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = first_tile(t, b), t1 = first_tile(t, b + 1);
-  for (i64 tile = t0, i = t0 < t1 ? find_item(t, t0) : 0; tile < t1; ++i) {
+  if (c.in_place) {
+    if (coef == 1.f || t0 >= t1) return;
+    i = find_item(t, t0);
+  }
+  for (i64 tile = t0; tile < t1; ++i) {
     const ScaleItem& it = t.item[i];
     i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
     if (end > t1) end = t1;
     if (end <= tile) continue;
-    if (!(coef == 1.f && it.g == it.out)) {
+    if (!(it.g == it.out && coef == 1.f)) {
       const Part p = part_of(it.w, tile, end);
       if (it.w.singles) {
         scale_singles(it, p, coef);
