@@ -534,13 +534,18 @@ __device__ __forceinline__ void scale_groups(const ScaleItem& it, const Part& p,
   TO* out = reinterpret_cast<TO*>(it.out);
   const Walk& w = it.w;
   i64 u = p.u0 + threadIdx.x;
-  if (w.per_row == w.units) {      // one row: as in norm_groups
+  if (w.per_row == w.units) {      // one row: as in norm_groups, but from its end
     const i64 first = w.phase != 0, end = (w.width + w.phase) / W < p.u1 ? (w.width + w.phase) / W : p.u1;
     const TG* g0 = g - w.phase;
     TO* out0 = out - w.phase;
-    if (u < first) u += THREADS;
-    for (; u + 3 * THREADS < end; u += 4 * THREADS) scale_some<TG, TO, 4>(g0 + u * W, out0 + u * W, coef);
-    for (; u < end; u += THREADS) scale_some<TG, TO, 1>(g0 + u * W, out0 + u * W, coef);
+    const i64 from = p.u0 < first ? first : p.u0;
+    i64 whole = end > from ? from + (end - from) / (4 * THREADS) * (4 * THREADS) : end;
+    for (u = whole + threadIdx.x; u < end; u += THREADS) scale_some<TG, TO, 1>(g0 + u * W, out0 + u * W, coef);
+    while (whole > from) {
+      whole -= 4 * THREADS;
+      u = whole + threadIdx.x;
+      scale_some<TG, TO, 4>(g0 + u * W, out0 + u * W, coef);
+    }
     u = threadIdx.x == 0 && p.u0 < first ? 0 : threadIdx.x == 32 && end >= first && end < p.u1 ? end : p.u1;
   }
   for (; u < p.u1; u += THREADS) {
@@ -588,10 +593,11 @@ __device__ __forceinline__ float norm_of_norms(const Clip& c) {
 // out = coefficient * G.  Where G itself would be multiplied by one nothing is read or written.
 template <int CAP>
 __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __grid_constant__ Table<ScaleItem, CAP> t, const Clip c) {
-  // the last blocks of the list first: what the norm's launch read last is still in L2
-  const i64 G = gridDim.x, b = G - 1 - blockIdx.x, t0 = first_tile(t, b), t1 = first_tile(t, b + 1);
+  // What the norm's launch read last is still in L2: a block of one wave has the tiles that it had there and walks them from the
+  // end; of many blocks those at the list's end come first.
+  const i64 b = gridDim.x - 1 - blockIdx.x, t0 = first_tile(t, b), t1 = first_tile(t, b + 1);
   // (The search and, further down, the first loads do not wait for the coefficient, except where it may say that nothing is to be done.)
-  i64 i = !c.in_place && t0 < t1 ? find_item(t, t0) : 0;
+  i64 i = !c.in_place && t0 < t1 ? find_item(t, t1 - 1) : 0;
   pdl_enter();
   float coef;
   if (c.coef != nullptr) {
@@ -607,13 +613,12 @@ __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __
   }
   if (c.in_place) {
     if (coef == 1.f || t0 >= t1) return;
-    i = find_item(t, t0);
+    i = find_item(t, t1 - 1);
   }
-  for (i64 tile = t0; tile < t1; ++i) {
+  for (i64 end = t1; end > t0; --i) {
     const ScaleItem& it = t.item[i];
-    i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
-    if (end > t1) end = t1;
-    if (end <= tile) continue;
+    const i64 tile = it.w.first > t0 ? it.w.first : t0;
+    if (tile >= end) continue;
     if (!(it.g == it.out && coef == 1.f)) {
       const Part p = part_of(it.w, tile, end);
       if (it.w.singles) {
@@ -624,7 +629,7 @@ __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __
         if (it.w.other_bf16) scale_groups<float, __nv_bfloat16>(it, p, coef); else scale_groups<float, float>(it, p, coef);
       }
     }
-    tile = end;
+    end = tile;
   }
 }
 
