@@ -14,7 +14,7 @@ namespace list {
 
 constexpr int THREADS = 256;
 constexpr int NORM_RESIDENT = 4, SCALE_RESIDENT = 4, ADAMW_RESIDENT = 3, LION_RESIDENT = 4;      // blocks per SM
-constexpr int MOST_NORM_BLOCKS = 1024, MOST_PARTS = MOST_NORM_BLOCKS + 500;      // blocks of a norm launch; with its arrays
+constexpr int MOST_NORM_BLOCKS = 1024, MOST_ARRAYS = 500, MOST_PARTS = MOST_NORM_BLOCKS + MOST_ARRAYS;      // of a norm launch
 constexpr int FEW_PARTS = 8;         // partial results of an array that one thread adds up
 constexpr int TILE_UNITS = 256;      // groups of a tile, one per thread
 constexpr int BATCH = 4;             // elements that a thread takes at once from an array that is walked one by one
@@ -68,6 +68,7 @@ struct Scratch {
   float coef;                    // clipping coefficient for the launch behind
   double carry;                  // sum (or maximum) over the launches of a list that takes several
   double pad[14];
+  int from[MOST_ARRAYS], upto[MOST_ARRAYS];      // with norms of each: an array's entries of `part`; zero between launches
   double part[MOST_PARTS];       // one entry per block and array that it touches
 };
 
@@ -102,15 +103,9 @@ struct Rule {
   int* status;                   // [0] bits, [1] cancelled steps
 };
 
-// The first tile of block b, and the block that takes a tile.
+// The first tile of block b.
 template <class Table>
 __device__ __forceinline__ i64 first_tile(const Table& t, i64 b) { return b * t.per + (b < t.rem ? b : t.rem); }
-template <class Table>
-__device__ __forceinline__ i64 owner_of(const Table& t, i64 tile) {
-  const i64 cut = t.rem * (t.per + 1);
-  return tile < cut ? row_of(tile, t.per + 1) : t.rem + row_of(tile - cut, t.per);
-}
-
 // The last array that starts at or before the tile.  Seven looks at a time: a look at the parameters is a round trip to memory
 // the first time, and these do not wait for one another.
 template <class Table>
@@ -330,13 +325,15 @@ __device__ __forceinline__ void norm_part(const NormItem& it, const Part& p, Acc
 
 // Global norm: every block leaves its partial sums, the last one to finish adds them up in the order of the blocks.
 // With `each` a block leaves one sum per array that it touches, at [block + array]: both grow along the tiles, so no two share an
-// entry and those of one array are neighbours.
+// entry and those of one array are neighbours.  The blocks that see an array begin and end note which they are.  (Finding that out
+// from the descriptors at the end, and one warp after another for arrays of many parts, cost 65 odd slices 1.7 us of 9.3.)
 template <int CAP, bool INF>
 __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __grid_constant__ Table<NormItem, CAP> t, const NormOut o) {
   __shared__ double red[THREADS / 32];
   __shared__ bool last;
   __shared__ double parts[MOST_PARTS];
-  __shared__ int from[CAP], upto[CAP];
+  __shared__ int from[CAP], upto[CAP], many[CAP], manies;
+  __shared__ double sums[CAP];
   const i64 G = gridDim.x, t0 = first_tile(t, blockIdx.x), t1 = first_tile(t, blockIdx.x + 1);
   i64 i = t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
@@ -345,13 +342,17 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
   Acc<INF> acc;
   for (i64 tile = t0; tile < t1; ++i) {
     const NormItem& it = t.item[i];
-    i64 end = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles;
-    if (end > t1) end = t1;
+    const i64 next = i + 1 < t.count ? t.item[i + 1].w.first : t.tiles, end = next < t1 ? next : t1;
     if (end <= tile) continue;
     norm_part(it, part_of(it.w, tile, end), acc);
     if (each) {
       const Acc<INF> r = block_reduce(acc, red);
-      if (threadIdx.x == 0) s->part[blockIdx.x + i] = r.kept();
+      if (threadIdx.x == 0) {
+        const int slot = (int)(blockIdx.x + i);
+        s->part[slot] = r.kept();
+        if (tile == it.w.first) s->from[i] = slot;
+        if (end == next) s->upto[i] = slot + 1;
+      }
       acc = Acc<INF>();
     }
     tile = end;
@@ -369,24 +370,25 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
   if (!last) return;
   Acc<INF> all;
   if (each) {
-    // Every partial result in one round trip.  Those of array i begin with the block that owns its first tile and end with the one
-    // that owns its last; a thread adds up a few, a warp many.
+    // everything in one round trip; then a thread adds up an array's few parts, a warp many
+    if (threadIdx.x == 0) manies = 0;
     for (int k = threadIdx.x; k < G + t.count; k += THREADS) parts[k] = __ldcg(&s->part[k]);
     for (int i = threadIdx.x; i < t.count; i += THREADS) {
-      const i64 f = t.item[i].w.first, l = (i + 1 < t.count ? t.item[i + 1].w.first : t.tiles) - 1;
-      from[i] = f <= l ? (int)owner_of(t, f) + i : 0;
-      upto[i] = f <= l ? (int)owner_of(t, l) + i + 1 : 0;
+      from[i] = __ldcg(&s->from[i]);
+      upto[i] = __ldcg(&s->upto[i]);      // (an empty array's are zero)
+      s->from[i] = 0;
+      s->upto[i] = 0;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < t.count; i += THREADS) {
-      if (upto[i] - from[i] > FEW_PARTS) continue;
+      if (upto[i] - from[i] > FEW_PARTS) { many[atomicAdd(&manies, 1)] = i; continue; }
       Acc<INF> a;
       for (int k = from[i]; k < upto[i]; ++k) a.merge(parts[k]);
-      o.each[i] = a.norm();
-      all.merge(a.kept());
+      sums[i] = a.kept();
     }
-    for (int i = threadIdx.x >> 5; i < t.count; i += THREADS / 32) {
-      if (upto[i] - from[i] <= FEW_PARTS) continue;
+    __syncthreads();
+    for (int m = threadIdx.x >> 5; m < manies; m += THREADS / 32) {
+      const int i = many[m];
       Acc<INF> a;
       for (int k = from[i] + (threadIdx.x & 31); k < upto[i]; k += 32) a.merge(parts[k]);
 #pragma unroll
@@ -394,7 +396,14 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
         if (INF) a.m = max(a.m, __shfl_xor_sync(0xffffffffu, a.m, d));
         else a.s += __shfl_xor_sync(0xffffffffu, a.s, d);
       }
-      if ((threadIdx.x & 31) == 0) { o.each[i] = a.norm(); all.merge(a.kept()); }
+      if ((threadIdx.x & 31) == 0) sums[i] = a.kept();
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < t.count; i += THREADS) {
+      Acc<INF> a;
+      a.merge(sums[i]);
+      o.each[i] = a.norm();
+      all.merge(sums[i]);
     }
   } else {
     for (i64 b = threadIdx.x; b < G; b += THREADS) all.merge(__ldcg(&s->part[b]));

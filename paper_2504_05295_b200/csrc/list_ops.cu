@@ -407,7 +407,7 @@ bool load(K kernel) {
 }  // namespace
 
 size_t scratch_bytes() { return (sizeof(Scratch) + 127) / 128 * 128; }
-static_assert(MANY_NORM <= MOST_PARTS - MOST_NORM_BLOCKS, "a launch's partial results fit");
+static_assert(MANY_NORM <= MOST_ARRAYS, "a launch's partial results fit");
 
 namespace {
 
