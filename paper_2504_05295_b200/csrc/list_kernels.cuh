@@ -78,14 +78,16 @@ struct NormOut {
   float* each;                   // optional: the norm of every array of this launch
   float* coef;                   // optional: min(1, max_norm / total)
   float max_norm;
+  int leave;                     // without `each`: the blocks' sums are left to the launch behind, which adds them up
   int use_carry, last;           // launches of one list: adds the carry of the one before; is the one that writes the total
   int* status;
 };
 
 struct Clip {
-  const float* coef;             // the coefficient on the device, or, where it is NULL,
-  const float* norms;            // the norms of parts of the whole, of which it is made
-  int count, inf;
+  const float* coef;             // the coefficient on the device, or one of the two of which it is made:
+  const double* sums;            // what the blocks of a norm's launch left
+  const float* norms;            // the norms of parts of the whole
+  int count, inf;                // ... and how many
   int in_place;                  // every array of the launch
   float max_norm;
   float* norm_out;
@@ -360,6 +362,7 @@ __global__ void __launch_bounds__(THREADS, NORM_RESIDENT) k_list_norm(const __gr
   if (!each) {
     const Acc<INF> r = block_reduce(acc, red);
     if (threadIdx.x == 0) s->part[blockIdx.x] = r.kept();
+    if (o.leave) return;
   }
   if (threadIdx.x == 0) {      // (it alone has written)
     __threadfence();
@@ -599,9 +602,22 @@ __device__ __forceinline__ float norm_of_norms(const Clip& c) {
   return a.norm();
 }
 
+// The norm from the sums of a norm's blocks, in every thread: in the order in which that launch would have added them up.
+template <bool INF>
+__device__ __forceinline__ float norm_of_sums(const Clip& c, double* red, float* shared_norm) {
+  Acc<INF> a;
+  for (int k = threadIdx.x; k < c.count; k += THREADS) a.merge(__ldcg(c.sums + k));
+  a = block_reduce(a, red);
+  if (threadIdx.x == 0) *shared_norm = a.norm();
+  __syncthreads();
+  return *shared_norm;
+}
+
 // out = coefficient * G.  Where G itself would be multiplied by one nothing is read or written.
 template <int CAP>
 __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __grid_constant__ Table<ScaleItem, CAP> t, const Clip c) {
+  __shared__ double red[THREADS / 32];
+  __shared__ float shared_norm;
   // What the norm's launch read last is still in L2: a block of one wave has the tiles that it had there and walks them from the
   // end; of many blocks those at the list's end come first.
   const i64 b = gridDim.x - 1 - blockIdx.x, t0 = first_tile(t, b), t1 = first_tile(t, b + 1);
@@ -612,7 +628,8 @@ __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __
   if (c.coef != nullptr) {
     coef = *c.coef;
   } else {
-    const float norm = c.inf ? norm_of_norms<true>(c) : norm_of_norms<false>(c);
+    const float norm = c.sums != nullptr ? (c.inf ? norm_of_sums<true>(c, red, &shared_norm) : norm_of_sums<false>(c, red, &shared_norm))
+                                         : (c.inf ? norm_of_norms<true>(c) : norm_of_norms<false>(c));
     coef = clip_coef(norm, c.max_norm);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
       if (!isfinite(norm)) atomicOr(c.status, DION_STATUS_NONFINITE);
