@@ -63,6 +63,7 @@ struct Table {
 };
 
 // What a norm launch leaves besides the caller's outputs (context scratch; its calls do not overlap).
+// Indexes found in it are in bounds whatever launch wrote them.
 struct Scratch {
   unsigned ticket;               // blocks that are done; zero between launches
   float coef;                    // clipping coefficient for the launch behind
@@ -84,10 +85,10 @@ struct NormOut {
 };
 
 struct Clip {
-  const float* coef;             // the coefficient on the device, or one of the two of which it is made:
-  const double* sums;            // what the blocks of a norm's launch left
-  const float* norms;            // the norms of parts of the whole
-  int count, inf;                // ... and how many
+  const float* coef;             // the coefficient on the device, or what it is made of:
+  const double* sums;            // what the blocks of a norm's launch left, or
+  const float* norms;            // the norms of parts of the whole,
+  int count, inf;                // and how many; which norm
   int in_place;                  // every array of the launch
   float max_norm;
   float* norm_out;
@@ -124,7 +125,7 @@ __device__ __forceinline__ int find_item(const Table& t, i64 tile) {
   }
   return lo;
 }
-static_assert(8 * 64 >= 500, "find_item reaches every array of a table");
+static_assert(8 * 64 >= MOST_ARRAYS, "find_item reaches every array of a table");
 
 __device__ __forceinline__ float load_as_float(const void* p, i64 at, int bf16) {
   return bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[at]) : reinterpret_cast<const float*>(p)[at];
@@ -493,6 +494,7 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 1) k_list_cluster(const __gri
       asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(to), "d"(a.kept()) : "memory");
     }
   }
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   Acc<INF> all;
 #pragma unroll
@@ -767,7 +769,7 @@ __device__ __forceinline__ void step_groups(const StepItem& it, const Part& p, c
 template <int CAP, bool ADAMW>
 __global__ void __launch_bounds__(THREADS, ADAMW ? ADAMW_RESIDENT : LION_RESIDENT) k_list_step(const __grid_constant__ Table<StepItem, CAP> t, const Rule r) {
   __shared__ float corr[2];
-  const i64 G = gridDim.x, t0 = first_tile(t, blockIdx.x), t1 = first_tile(t, blockIdx.x + 1);
+  const i64 t0 = first_tile(t, blockIdx.x), t1 = first_tile(t, blockIdx.x + 1);
   i64 i = t0 < t1 ? find_item(t, t0) : 0;
   pdl_enter();
   const float s = r.scale != nullptr ? *r.scale : 1.f;

@@ -115,6 +115,21 @@ def test_norm_of_long_lists(opt, count):
     assert float(total) == norm64(ts, "inf")
 
 
+def test_norm_of_nothing(opt):
+    empty, out, each, coef = torch.zeros(0, device="cuda"), scalar(-1), torch.full((40,), -1.0, device="cuda"), scalar(-1)
+    for kind in (2, "inf"):
+        opt.grad_norm(binding.grad_list([empty] * 40), kind, norm_out=out, each_out=each, max_norm=1.0, coef_out=coef)
+        assert float(out) == 0.0 and float(coef) == 1.0 and not bool(each.any())
+        opt.clip_grads(binding.grad_list([empty] * 140), 1.0, norm_type=kind, norm_out=out, coef_out=coef)
+        assert float(out) == 0.0 and float(coef) == 1.0
+        opt.clip_grads(binding.grad_list([empty] * 140), 1.0, norms=torch.full((3,), 2.0, device="cuda"), norm_type=kind, coef_out=coef)
+        assert abs(float(coef) - (0.5 if kind == "inf" else 0.5 / math.sqrt(3))) <= COEF
+    none = binding.param_list([binding.param_desc(empty, empty, empty, empty)] * 30)
+    opt.adamw_step(none, 0.1, 1)
+    opt.lion_step(none, 0.1)
+    assert opt.get_status() == (0, 0)
+
+
 def test_norm_counts_an_array_twice(opt):
     t, out = torch.randn(1000, generator=gen(0), device="cuda"), scalar()
     opt.grad_norm(binding.grad_list([t, t]), norm_out=out)
