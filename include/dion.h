@@ -286,8 +286,9 @@ int dion_shard_finish(dion_ctx* ctx, const dion_matrix* a, int64_t n_total, cons
  * A list is a HOST array of descriptors holding DEVICE pointers, read before the call returns; one call takes any number of
  * arrays of any sizes and types in one launch per 250 (AdamW, Lion), 400 (scaling) or 500 (norm) of them.  An array is
  * rows x cols with a leading dimension in elements (a vector is one row; rows or cols may be 0).  Pointers need the alignment
- * of their element type only; the arrays of an entry whose addresses and leading dimensions agree modulo 8 elements move in
- * pieces of 8 elements, others (and matrices of fewer than 32 columns that are not dense) element by element.
+ * of their element type only; the arrays of an entry that are written move in pieces of 8 elements where their addresses and
+ * leading dimensions agree modulo 8 elements, and the gradient too where it agrees with them; others (and matrices of fewer than
+ * 32 columns that are not dense) element by element.
  *
  * Nothing that a call writes may be touched twice by it: neither the same array twice in a list nor overlapping ones
  * (DION_ERR_ALIAS); column slices of one matrix do not overlap.  dion_grad_norm takes an array twice and counts it twice.

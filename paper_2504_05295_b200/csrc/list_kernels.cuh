@@ -23,8 +23,10 @@ constexpr int W = 8;                 // elements of a group: 32 bytes of fp32 (o
 // How an array is walked.  Its rows are cut into groups of W elements at multiples of W elements of the ADDRESS, which is the same
 // cut for all arrays of an item: what lies wholly in its row is one access per array, what hangs over a row's end goes element
 // by element.  A row of `width` elements has groups at up to (width + 14) / 8 places, and each row is given that many.
-// One by one go items whose arrays' addresses (or leading dimensions) do not agree modulo W, and narrow rows, most of whose
-// groups would hang over an end.
+// The cut is that of the arrays that are written; a gradient that lies apart from them modulo W (or has another leading
+// dimension) is read by the element, out of L1 after the first of a group (67M parameters, gradient in bf16: AdamW 587 us one
+// by one, 258 so; scaling into another buffer 315 and 61).
+// One by one go items whose written arrays do not agree, and narrow rows, most of whose groups would hang over an end.
 struct Walk {
   i64 first;                     // its first tile
   i64 units, per_row;            // groups, or elements; of these in a row
@@ -32,6 +34,7 @@ struct Walk {
   uint8_t phase, shift;          // address of row 0 and leading dimension, in elements modulo W
   bool singles;                  // one by one
   bool g_bf16, other_bf16;       // types: of G; of the result or the moment
+  bool g_apart;                  // G is not cut as the others are
 };
 struct NormItem {
   Walk w;
@@ -181,6 +184,10 @@ __device__ __forceinline__ void load_group(const T* p, float (&x)[W], int lo, in
   if (lo == 0 && hi == W) load_vec(p, x); else load_part(p, x, lo, hi);
 }
 template <typename T>
+__device__ __forceinline__ void load_gradient(const T* p, float (&x)[W], int lo, int hi, bool apart) {
+  if (lo == 0 && hi == W && !apart) load_vec(p, x); else load_part(p, x, lo, hi);
+}
+template <typename T>
 __device__ __forceinline__ void store_group(T* p, const float (&x)[W], int lo, int hi) {
   if (lo == 0 && hi == W) store_vec(p, x); else store_part(p, x, lo, hi);
 }
@@ -209,6 +216,41 @@ __device__ __forceinline__ Spot group_at(const Walk& w, i64 u) {
   s.col = (u - s.row * w.per_row) * W - ((w.phase + (uint32_t)s.row * w.shift) & (W - 1));
   s.lo = s.col < 0 ? (int)-s.col : 0;
   s.hi = w.width - s.col < W ? (int)(w.width - s.col) : W;      // (below lo: a place that this row does not fill)
+  return s;
+}
+
+// Of a block's part, the groups of one row: wide rows (and dense arrays, which are one) are walked row by row, since the arithmetic
+// of group_at is several times that of a norm.  All groups are whole but the row's first (if the row starts inside one) and its
+// last; `first` and `last` are theirs if the part has them, else -1.
+constexpr int WIDE = THREADS;        // groups of a wide row
+struct RowRun {
+  i64 row, col;                      // the row, and the column of its group 0
+  i64 lo, hi;                        // whole groups
+  i64 first, last;
+  i64 end;                           // of the part: where the next row goes on
+};
+__device__ __forceinline__ bool by_rows(const Walk& w) { return w.per_row >= WIDE || w.per_row == w.units; }
+__device__ __forceinline__ RowRun row_run(const Walk& w, i64 u, i64 u1) {
+  RowRun r;
+  r.row = row_at(w, u);
+  const i64 u0 = r.row * w.per_row, k0 = u - u0;
+  r.end = u0 + w.per_row < u1 ? u0 + w.per_row : u1;
+  const i64 k1 = r.end - u0, phase = (w.phase + (uint32_t)r.row * w.shift) & (W - 1), whole = (w.width + phase) / W;
+  r.col = -phase;
+  r.lo = k0 == 0 && phase != 0 ? 1 : k0;
+  r.hi = k1 < whole ? k1 : whole;
+  r.first = k0 == 0 && phase != 0 ? 0 : -1;
+  r.last = whole >= r.lo && whole < k1 && whole * W < w.width + phase ? whole : -1;
+  return r;
+}
+// The row's first group is thread 0's, its last one another's.
+__device__ __forceinline__ i64 end_group(const RowRun& r) { return threadIdx.x == 0 ? r.first : threadIdx.x == 32 ? r.last : -1; }
+__device__ __forceinline__ Spot spot_in(const Walk& w, const RowRun& r, i64 k) {
+  Spot s;
+  s.row = r.row;
+  s.col = r.col + k * W;
+  s.lo = s.col < 0 ? (int)-s.col : 0;
+  s.hi = w.width - s.col < W ? (int)(w.width - s.col) : W;
   return s;
 }
 
@@ -277,33 +319,39 @@ template <bool INF, typename T>
 __device__ __forceinline__ void norm_groups(const NormItem& it, const Part& p, Acc<INF>& acc) {
   const T* g = reinterpret_cast<const T*>(it.g);
   const Walk& w = it.w;
-  i64 u = p.u0 + threadIdx.x;
-  if (w.per_row == w.units) {
-    // one row: all but its first and last groups are whole, and four loads are in flight per thread
-    const i64 first = w.phase != 0, end = (w.width + w.phase) / W < p.u1 ? (w.width + w.phase) / W : p.u1;
-    const T* g0 = g - w.phase;
-    if (u < first) u += THREADS;
-    for (; u + 3 * THREADS < end; u += 4 * THREADS) {
-      float x[4][W];
+  if (by_rows(w)) {
+    for (i64 u = p.u0; u < p.u1;) {
+      const RowRun r = row_run(w, u, p.u1);
+      const T* g0 = g + r.row * it.ldg + r.col;
+      i64 k = r.lo + threadIdx.x;
+      for (; k + 3 * THREADS < r.hi; k += 4 * THREADS) {      // four loads in flight per thread
+        float x[4][W];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) load_vec(g0 + (u + k * THREADS) * W, x[k]);
+        for (int q = 0; q < 4; ++q) load_vec(g0 + (k + q * THREADS) * W, x[q]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) acc.add(x[k]);
+        for (int q = 0; q < 4; ++q) acc.add(x[q]);
+      }
+      for (; k < r.hi; k += THREADS) {
+        float x[W];
+        load_vec(g0 + k * W, x);
+        acc.add(x);
+      }
+      k = end_group(r);
+      if (k >= 0) {
+        const Spot s = spot_in(w, r, k);
+        float x[W];
+        load_part(g0 + k * W, x, s.lo, s.hi);
+        acc.add(x);
+      }
+      u = r.end;
     }
-    for (; u < end; u += THREADS) {
-      float x[W];
-      load_vec(g0 + u * W, x);
-      acc.add(x);
-    }
-    // (thread 0 takes the first group, another one the last)
-    u = threadIdx.x == 0 && p.u0 < first ? 0 : threadIdx.x == 32 && end >= first && end < p.u1 ? end : p.u1;
+    return;
   }
-  for (; u < p.u1; u += THREADS) {
+  for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) {
     const Spot s = group_at(w, u);
     float x[W];
     load_group(g + s.row * it.ldg + s.col, x, s.lo, s.hi);
     acc.add(x);
-    if (w.per_row == w.units) break;
   }
 }
 
@@ -466,8 +514,8 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 1) k_list_cluster(const __gri
     } else if (u < it.w.units) {
       const Spot at = group_at(it.w, u);
       const i64 e = at.row * it.ldg + at.col;
-      if (it.w.g_bf16) load_group(reinterpret_cast<const __nv_bfloat16*>(it.g) + e, x[k], at.lo, at.hi);
-      else load_group(reinterpret_cast<const float*>(it.g) + e, x[k], at.lo, at.hi);
+      if (it.w.g_bf16) load_gradient(reinterpret_cast<const __nv_bfloat16*>(it.g) + e, x[k], at.lo, at.hi, it.w.g_apart);
+      else load_gradient(reinterpret_cast<const float*>(it.g) + e, x[k], at.lo, at.hi, it.w.g_apart);
     }
   }
 #pragma unroll
@@ -529,11 +577,13 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 1) k_list_cluster(const __gri
   }
 }
 
-template <typename TG, typename TO, int N>
-__device__ __forceinline__ void scale_some(const TG* g, TO* out, float coef) {      // N vectors, THREADS apart
+template <typename TG, typename TO, int N, bool APART = false>
+__device__ __forceinline__ void scale_some(const TG* g, TO* out, float coef) {      // N groups, THREADS apart
   float x[N][W];
 #pragma unroll
-  for (int k = 0; k < N; ++k) load_vec(g + k * THREADS * W, x[k]);
+  for (int k = 0; k < N; ++k) {
+    if (APART) load_part(g + k * THREADS * W, x[k], 0, W); else load_vec(g + k * THREADS * W, x[k]);
+  }
 #pragma unroll
   for (int k = 0; k < N; ++k) {
 #pragma unroll
@@ -547,30 +597,35 @@ __device__ __forceinline__ void scale_groups(const ScaleItem& it, const Part& p,
   const TG* g = reinterpret_cast<const TG*>(it.g);
   TO* out = reinterpret_cast<TO*>(it.out);
   const Walk& w = it.w;
-  i64 u = p.u0 + threadIdx.x;
-  if (w.per_row == w.units) {      // one row: as in norm_groups, but from its end
-    const i64 first = w.phase != 0, end = (w.width + w.phase) / W < p.u1 ? (w.width + w.phase) / W : p.u1;
-    const TG* g0 = g - w.phase;
-    TO* out0 = out - w.phase;
-    const i64 from = p.u0 < first ? first : p.u0;
-    i64 whole = end > from ? from + (end - from) / (4 * THREADS) * (4 * THREADS) : end;
-    for (u = whole + threadIdx.x; u < end; u += THREADS) scale_some<TG, TO, 1>(g0 + u * W, out0 + u * W, coef);
-    while (whole > from) {
-      whole -= 4 * THREADS;
-      u = whole + threadIdx.x;
-      scale_some<TG, TO, 4>(g0 + u * W, out0 + u * W, coef);
-    }
-    u = threadIdx.x == 0 && p.u0 < first ? 0 : threadIdx.x == 32 && end >= first && end < p.u1 ? end : p.u1;
-  }
-  for (; u < p.u1; u += THREADS) {
-    const Spot s = group_at(w, u);
+  const auto partly = [&](const Spot& s) {
     float x[W];
-    load_group(g + s.row * it.ldg + s.col, x, s.lo, s.hi);
+    load_gradient(g + s.row * it.ldg + s.col, x, s.lo, s.hi, w.g_apart);
 #pragma unroll
     for (int k = 0; k < W; ++k) x[k] *= coef;
     store_group(out + s.row * it.ldo + s.col, x, s.lo, s.hi);
-    if (w.per_row == w.units) break;
+  };
+  if (by_rows(w)) {      // as in norm_groups, but every row from its end
+    for (i64 u = p.u0; u < p.u1;) {
+      const RowRun r = row_run(w, u, p.u1);
+      const TG* g0 = g + r.row * it.ldg + r.col;
+      TO* out0 = out + r.row * it.ldo + r.col;
+      if (w.g_apart) {
+        for (i64 k = r.lo + threadIdx.x; k < r.hi; k += THREADS) scale_some<TG, TO, 1, true>(g0 + k * W, out0 + k * W, coef);
+      } else {
+        i64 fours = r.hi > r.lo ? r.lo + (r.hi - r.lo) / (4 * THREADS) * (4 * THREADS) : r.hi;
+        for (i64 k = fours + threadIdx.x; k < r.hi; k += THREADS) scale_some<TG, TO, 1>(g0 + k * W, out0 + k * W, coef);
+        while (fours > r.lo) {
+          fours -= 4 * THREADS;
+          scale_some<TG, TO, 4>(g0 + (fours + threadIdx.x) * W, out0 + (fours + threadIdx.x) * W, coef);
+        }
+      }
+      const i64 k = end_group(r);
+      if (k >= 0) partly(spot_in(w, r, k));
+      u = r.end;
+    }
+    return;
   }
+  for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) partly(group_at(w, u));
 }
 
 __device__ __forceinline__ void scale_singles(const ScaleItem& it, const Part& p, float coef) {
@@ -726,9 +781,9 @@ __device__ __forceinline__ void step_singles(const StepItem& it, const Part& p, 
 
 template <bool ADAMW, typename TG, typename TM>
 __device__ __forceinline__ void step_group(const StepItem& it, const Rule& r, float inv1, float inv2, float s, float* px, const TG* pg, TM* pm, float* pv,
-                                           __nv_bfloat16* p16, int lo, int hi) {
+                                           __nv_bfloat16* p16, int lo, int hi, bool apart) {
   float x[W], m[W], v[W], g[W];
-  load_group(pg, g, lo, hi);
+  load_gradient(pg, g, lo, hi, apart);
   load_group(pm, m, lo, hi);
   if (ADAMW) load_group(pv, v, lo, hi);
   load_group(px, x, lo, hi);
@@ -748,22 +803,28 @@ __device__ __forceinline__ void step_groups(const StepItem& it, const Part& p, c
   const TG* G = reinterpret_cast<const TG*>(it.G);
   TM* M = reinterpret_cast<TM*>(it.M);
   const Walk& w = it.w;
-  i64 u = p.u0 + threadIdx.x;
-  if (w.per_row == w.units) {      // one row: as in norm_groups
-    const i64 first = w.phase != 0, end = (w.width + w.phase) / W < p.u1 ? (w.width + w.phase) / W : p.u1;
-    if (u < first) u += THREADS;
-    for (; u < end; u += THREADS) {
-      const i64 e = u * W - w.phase;
-      step_group<ADAMW>(it, r, inv1, inv2, s, it.X + e, G + e, M + e, it.V + e, it.X16 + e, 0, W);
-    }
-    u = threadIdx.x == 0 && p.u0 < first ? 0 : threadIdx.x == 32 && end >= first && end < p.u1 ? end : p.u1;
-  }
-  for (; u < p.u1; u += THREADS) {
-    const Spot at = group_at(w, u);
+  const auto partly = [&](const Spot& at) {
     step_group<ADAMW>(it, r, inv1, inv2, s, it.X + at.row * it.ldx + at.col, G + at.row * it.ldg + at.col, M + at.row * it.ldm + at.col,
-                      it.V + at.row * it.ldv + at.col, it.X16 + at.row * it.ldx16 + at.col, at.lo, at.hi);
-    if (w.per_row == w.units) break;
+                      it.V + at.row * it.ldv + at.col, it.X16 + at.row * it.ldx16 + at.col, at.lo, at.hi, w.g_apart);
+  };
+  if (w.per_row == w.units) {      // one row: as in norm_groups.  (Other rows are bound by memory as they are.)
+    const RowRun run = row_run(w, p.u0, p.u1);
+    if (w.g_apart) {
+      for (i64 k = run.lo + threadIdx.x; k < run.hi; k += THREADS) {
+        const i64 e = k * W + run.col;
+        step_group<ADAMW>(it, r, inv1, inv2, s, it.X + e, G + e, M + e, it.V + e, it.X16 + e, 0, W, true);
+      }
+    } else {
+      for (i64 k = run.lo + threadIdx.x; k < run.hi; k += THREADS) {
+        const i64 e = k * W + run.col;
+        step_group<ADAMW>(it, r, inv1, inv2, s, it.X + e, G + e, M + e, it.V + e, it.X16 + e, 0, W, false);
+      }
+    }
+    const i64 k = end_group(run);
+    if (k >= 0) partly(spot_in(w, run, k));
+    return;
   }
+  for (i64 u = p.u0 + threadIdx.x; u < p.u1; u += THREADS) partly(group_at(w, u));
 }
 
 template <int CAP, bool ADAMW>

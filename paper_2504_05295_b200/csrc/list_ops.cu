@@ -207,7 +207,8 @@ inline int shift_of(int dtype) { return dtype == DION_BF16 ? 1 : 2; }
 
 constexpr i64 NARROW = 32;      // rows of fewer elements go one by one
 
-// How arrays of rows x cols are walked together, and their tiles behind the `tiles` so far.
+// How arrays of rows x cols are walked together, and their tiles behind the `tiles` so far.  The first of the arrays is the
+// gradient, whose addresses need not agree with those of the others.
 template <size_t N>
 Walk plan(i64 rows, i64 cols, int g_dtype, int other_dtype, const Array (&a)[N], i64* tiles) {
   Walk w = {};
@@ -216,12 +217,15 @@ Walk plan(i64 rows, i64 cols, int g_dtype, int other_dtype, const Array (&a)[N],
   if (rows == 0 || cols == 0) return w;
   bool agree = true, dense = true;
   int phase = -1, shift = 0;
-  for (const Array& x : a) {
+  for (size_t k = N; k-- > 0;) {
+    const Array& x = a[k];
     if (x.p == nullptr) continue;
     const int ph = (int)((uintptr_t)x.p >> x.shift) & (W - 1), sh = (int)x.ld & (W - 1);
-    agree = agree && (phase < 0 || (ph == phase && (rows == 1 || sh == shift)));
-    phase = ph; shift = sh;
+    const bool same = phase < 0 || (ph == phase && (rows == 1 || sh == shift));
     dense = dense && (rows == 1 || x.ld == cols);
+    if (k == 0 && !same) { w.g_apart = true; break; }
+    agree = agree && same;
+    phase = ph; shift = sh;
   }
   if (dense) { cols *= rows; rows = 1; }
   w.width = cols;
@@ -396,7 +400,7 @@ int step(const Where& w, const dion_param* list, int count, Rule r, float lr) {
       it->X16 = (__nv_bfloat16*)a.X16; it->ldx16 = a.ldx16;
       it->lr = lr * a.lr_scale;
       it->keep = (float)(1.0 - (double)lr * a.lr_scale * a.weight_decay);
-      const Array arrays[] = {{it->X, a.ldx, 2}, {a.G, a.ldg, shift_of(a.g_dtype)}, {a.M, a.ldm, shift_of(a.m_dtype)}, {it->V, a.ldv, 2}, {it->X16, a.ldx16, 1}};
+      const Array arrays[] = {{a.G, a.ldg, shift_of(a.g_dtype)}, {it->X, a.ldx, 2}, {a.M, a.ldm, shift_of(a.m_dtype)}, {it->V, a.ldv, 2}, {it->X16, a.ldx16, 1}};
       it->w = plan(rows, cols, a.g_dtype, a.m_dtype, arrays, &t.tiles);
     }
     LIST_TRY(by_count(t, [&](auto& table) {

@@ -432,7 +432,8 @@ def check_step(before, after, adamw, lr, b1, b2, eps, t, s, lr_scale, wd):
 
 @pytest.mark.parametrize("adamw", [True, False], ids=["adamw", "lion"])
 @pytest.mark.parametrize("copy", [False, True])
-@pytest.mark.parametrize("lies", [[PLAIN], [SHIFTED], [SLICED], [ALIGNED_SLICES], [PLAIN, SHIFTED], [PLAIN, ALIGNED_SLICES, SLICED]])
+@pytest.mark.parametrize("lies", [[PLAIN], [SHIFTED], [SLICED], [ALIGNED_SLICES], [PLAIN, SHIFTED], [PLAIN, ALIGNED_SLICES, SLICED],
+                                  [PLAIN, SHIFTED, PLAIN, PLAIN, PLAIN], [SLICED, PLAIN, SLICED, SLICED, SLICED], [SHIFTED, ALIGNED_SLICES, SHIFTED, SHIFTED, SHIFTED]])
 @pytest.mark.parametrize("g,m", [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
 def test_step(opt, adamw, g, m, lies, copy):
     made = make_params(SHAPES, g, m, lies, copy, 100, adamw)
