@@ -722,10 +722,11 @@ __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __
 }
 
 // sign(beta1 m + (1 - beta1) s g).  A fp32 evaluation is off by less than 2^-22 of the gradient's term (its three roundings and
-// those of the factors) and 2^-23 of the sum; where the terms cancel further than 2^-20 the sum is taken in 64 bits.
+// those of the factors), 2^-23 of the sum and, where a product falls below 2^-126, 2^-148; where the terms cancel further than
+// 2^-20, and where the sum is below 2^-126, it is taken in 64 bits.
 __device__ __forceinline__ float lion_sign(const Rule& r, float m, float g, float s) {
   const float a = r.c1 * (s * g), c = fmaf(r.b1, m, a);
-  if (fabsf(c) <= 9.5367432e-7f * fabsf(a)) {
+  if (fabsf(c) <= fmaf(9.5367432e-7f, fabsf(a), 1.1754944e-38f)) {
     const double d = r.beta1 * (double)m + (1.0 - r.beta1) * ((double)s * (double)g);
     return d > 0.0 ? 1.f : d < 0.0 ? -1.f : 0.f;
   }
