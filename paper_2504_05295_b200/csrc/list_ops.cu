@@ -544,6 +544,13 @@ NormOut norm_out_of(const Where& w, float max_norm, float* norm_out, float* coef
   return o;
 }
 
+// hi is the largest float below beta, lo the rest.
+Beta split(double beta) {
+  float hi = (float)beta;
+  if (hi > 0.f && (double)hi >= beta) hi = nextafterf(hi, 0.f);
+  return {hi, (float)(beta - (double)hi)};
+}
+
 }  // namespace
 
 int grad_norm(const Where& w, const dion_grad* list, int count, int norm_type, float max_norm, float* norm_out, float* each_out,
@@ -583,7 +590,9 @@ int param_step(const Where& w, bool adamw, const dion_param* list, int count, co
   Rule r = {};
   r.beta1 = rule->beta1; r.beta2 = rule->beta2;
   r.b1 = (float)rule->beta1; r.c1 = (float)(1.0 - rule->beta1);
-  r.b2 = (float)rule->beta2; r.c2 = (float)(1.0 - rule->beta2);
+  const double of_m = adamw ? rule->beta1 : rule->beta2;
+  r.m = split(of_m); r.cm = (float)(1.0 - of_m);
+  r.v = split(rule->beta2); r.cv = (float)(1.0 - rule->beta2);
   r.eps = (float)rule->eps;
   r.step_dev = adamw ? rule->step_dev : nullptr;
   if (adamw && rule->step_dev == nullptr) {
