@@ -291,7 +291,8 @@ int dion_shard_finish(dion_ctx* ctx, const dion_matrix* a, int64_t n_total, cons
  * 32 columns that are not dense) element by element.
  *
  * Nothing that a call writes may be touched twice by it: neither the same array twice in a list nor overlapping ones
- * (DION_ERR_ALIAS); column slices of one matrix do not overlap.  dion_grad_norm takes an array twice and counts it twice.
+ * (DION_ERR_ALIAS); rows and columns of one matrix, and a number between two rows of an array, share no element and do not
+ * overlap.  dion_grad_norm takes an array twice and counts it twice.
  * The calls are asynchronous on `cuda_stream`, allocate nothing, leave the calling thread's current device as it was and may
  * be captured into a CUDA graph (the host values of the call, lr and step among them, are those of the capture).  A captured
  * call has scratch of its own, so graphs of one context may run side by side (the last 63 captured calls over lists, that is:

@@ -4,6 +4,7 @@
 #include <string.h>
 #include <algorithm>
 #include <new>
+#include <numeric>
 #include <type_traits>
 
 #include "list_api.cuh"
@@ -88,6 +89,7 @@ int check_array(const void* p, i64 rows, i64 cols, i64 ld, int size) {
 struct Range {
   uintptr_t begin, end;
   uintptr_t width, pitch;      // pitch 0: one row
+  uintptr_t rows;
   bool written;
 };
 Range range_of(const void* p, i64 rows, i64 cols, i64 ld, int size, bool written) {
@@ -96,18 +98,25 @@ Range range_of(const void* p, i64 rows, i64 cols, i64 ld, int size, bool written
   r.width = (uintptr_t)(cols * size);
   r.pitch = rows > 1 && ld != cols ? (uintptr_t)(ld * size) : 0;
   if (r.pitch == 0) r.width = (uintptr_t)(rows * cols * size);
+  r.rows = r.pitch == 0 ? 1 : (uintptr_t)rows;
   r.end = r.begin + (r.pitch == 0 ? r.width : (uintptr_t)(rows - 1) * r.pitch + r.width);
   r.written = written;
   return r;
 }
+// The first row of r that ends behind p.
+uintptr_t row_behind(const Range& r, uintptr_t p) { return p < r.begin + r.width ? 0 : r.pitch == 0 ? 1 : (p - r.begin - r.width) / r.pitch + 1; }
+// Whether any byte belongs to both.  The rows of one are looked up in the other, as far as the two lie beside one another: the
+// first, which may begin before the other does, and as many more as begin at different places within the other's pitch.
 bool conflict(const Range& a, const Range& b) {
   if ((!a.written && !b.written) || a.begin >= b.end || b.begin >= a.end) return false;
-  if (a.pitch != 0 && a.pitch == b.pitch) {      // two column slices of one matrix
-    const Range &lo = a.begin <= b.begin ? a : b, &hi = a.begin <= b.begin ? b : a;
-    const uintptr_t off = (hi.begin - lo.begin) % a.pitch;
-    return !(off >= lo.width && off + hi.width <= a.pitch);
+  const Range &x = b.pitch == 0 ? b : a, &y = b.pitch == 0 ? a : b;      // (if one of them is a single row, x is)
+  const uintptr_t first = row_behind(x, y.begin), places = y.pitch == 0 ? 0 : y.pitch / std::gcd(x.pitch, y.pitch);
+  for (uintptr_t i = first; i < x.rows && i - first <= places; ++i) {
+    const uintptr_t from = x.begin + i * x.pitch;
+    if (from >= y.end) break;
+    if (y.begin + row_behind(y, from) * y.pitch < from + x.width) return true;      // (from < y.end: there is such a row)
   }
-  return true;
+  return false;
 }
 
 // Ranges of one kind (all X, all G, ...), as runs of ranges that follow one another at once or after a short gap: lists are often
