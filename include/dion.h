@@ -353,7 +353,7 @@ typedef struct {
 
 typedef struct {
   double beta1, beta2;  /* in [0, 1)                                                        */
-  double eps;           /* AdamW: >= 0                                                      */
+  double eps;           /* AdamW: 0, or from 2^-126 to 2^125                                */
   int64_t step;         /* AdamW: the number t of this step, from 1                         */
   const int64_t* step_dev;  /* optional, AdamW: DEVICE, holds t instead of `step` (for captured steps; a step with t < 1 is
                            cancelled)                                                       */

@@ -742,7 +742,8 @@ __device__ __forceinline__ float lion_sign(const Rule& r, float m, float g, floa
 
 // The update's root and quotient need not be the nearest numbers (relative errors 2^-23 and 2^-22, of an update that is a
 // thousandth of X or so); the correctly rounded ones are most of a short list's instructions (65 odd slices 11.9 us against 8.2).
-// (Divisors: below 2^-126 only as zero, where the quotient is that of zero, and never near 2^126.)
+// (Divisors: eps is 0 or between 2^-126 and 2^125, V's root 0 or between 2^-75 and 2^64, so their sum is below 2^-126 only as
+// zero, where eps is, and below 2^126; or V is infinite and the quotient zero.)
 __device__ __forceinline__ float sqrt_approx(float x) {
   float y;
   asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -512,7 +512,9 @@ int check_clip(const dion_grad* list, int count, float max_norm, int norm_type, 
 int check_step(bool adamw, const dion_param* list, int count, const dion_rule* rule, float lr) {
   if (count < 0 || (count > 0 && list == nullptr) || rule == nullptr || !isfinite(lr)) return DION_ERR_INVALID;
   if (!(rule->beta1 >= 0.0 && rule->beta1 < 1.0) || !(rule->beta2 >= 0.0 && rule->beta2 < 1.0)) return DION_ERR_INVALID;
-  if (adamw && (!(rule->eps >= 0.0) || !isfinite(rule->eps) || (rule->step_dev == nullptr && rule->step < 1))) return DION_ERR_INVALID;
+  // (the step's quotient is within its bound for divisors in this range; below it V's root alone is never, but zero)
+  if (adamw && rule->eps != 0.0 && !(rule->eps >= 0x1p-126 && rule->eps <= 0x1p125)) return DION_ERR_INVALID;
+  if (adamw && rule->step_dev == nullptr && rule->step < 1) return DION_ERR_INVALID;
   if ((uintptr_t)rule->step_dev & 7) return DION_ERR_ALIGN;
   LIST_TRY(check_floats(rule->grad_scale));
   Runs kind[7];
