@@ -2595,9 +2595,17 @@ int dion_init(dion_ctx** out, const dion_config* cfg) {
   c->flow_ctl = c->dev_ints + 8 + MAX_FLAG_SLOTS * OS_SLOT_INTS + 24;      // (128-byte aligned)
   c->flow_ctl_cap = FLOW_CTL_INTS;
   c->list_scratch = (char*)p + ctl_bytes;
-  if (cudaMemset(p, 0, int_bytes) != cudaSuccess) { cudaFree(p); delete c; return DION_ERR_CUDA; }
-  if (configure_kernels() != DION_OK || list::configure() != DION_OK) { cudaFree(p); delete c; return DION_ERR_CUDA; }
   if (cudaStreamCreateWithFlags(&c->side, cudaStreamNonBlocking) != cudaSuccess) { cudaGetLastError(); c->side = nullptr; }
+  // zero before this returns: on the default stream it would come behind whatever is queued there, and a call on another stream
+  // could run before it
+  if (cudaMemsetAsync(p, 0, int_bytes, c->side) != cudaSuccess || cudaStreamSynchronize(c->side) != cudaSuccess ||
+      configure_kernels() != DION_OK || list::configure() != DION_OK) {
+    cudaGetLastError();
+    if (c->side != nullptr) cudaStreamDestroy(c->side);
+    cudaFree(p);
+    delete c;
+    return DION_ERR_CUDA;
+  }
   // graph replay of small steps: a capture stream and the scalars the graphs read; off if either cannot be had
   umma::pair_clusters(c->sm_count);      // (asked once per device, outside any capture)
   {
