@@ -310,8 +310,9 @@ typedef struct {
   int out_dtype;
 } dion_grad;
 
-/* Norm of all elements of the list: the 2-norm or the largest magnitude.  Sums are held in 64 bits, so neither large nor small
- * gradients overflow or vanish in their squares.  Outputs are DEVICE floats, each optional but not all three NULL:
+/* Norm of all elements of the list: the 2-norm or the largest magnitude.  Up to eight neighbours' squares are added in fp32 where
+ * their sum is in its range, everything else in 64 bits: a 2-norm of 2^-126 or more is within 5 * 2^-24 of its value, and neither
+ * large nor small gradients overflow or vanish in their squares.  Outputs are DEVICE floats, each optional but not all three NULL:
  *   norm_out   the norm (0 of an empty list)
  *   each_out   `count` norms, one per array
  *   coef_out   min(1, max_norm / norm), what dion_clip_grads would multiply by, for dion_rule.grad_scale (max_norm >= 0, may be
@@ -364,7 +365,7 @@ typedef struct {
 
 /* One AdamW step on a list of parameters:  g = s G,  M <- beta1 M + (1 - beta1) g,  V <- beta2 V + (1 - beta2) g^2,
  * X <- (1 - lr wd) X - lr (M / (1 - beta1^t)) / (sqrt(V / (1 - beta2^t)) + eps), lr being lr * lr_scale.  The arithmetic is
- * fp32 (root and quotient within 2^-22).  A NaN or Inf in G stays in its element; with eps = 0 an element whose moments are both
+ * fp32 (root and quotient within 2^-22; the betas within 2^-47, so that moments settle where the formula does).  A NaN or Inf in G stays in its element; with eps = 0 an element whose moments are both
  * zero divides zero by zero. */
 int dion_adamw_step(dion_ctx* ctx, const dion_param* list, int count, const dion_rule* rule, float lr, void* cuda_stream);
 

@@ -25,7 +25,7 @@ constexpr int W = 8;                 // elements of a group: 32 bytes of fp32 (o
 // by element.  A row of `width` elements has groups at up to (width + 14) / 8 places, and each row is given that many.
 // The cut is that of the arrays that are written; a gradient that lies apart from them modulo W (or has another leading
 // dimension) is read by the element, out of L1 after the first of a group (67M parameters, gradient in bf16: AdamW 587 us one
-// by one, 258 so; scaling into another buffer 315 and 61).
+// by one, 258 so; scaling into another buffer 315 and 62).
 // One by one go items whose written arrays do not agree, and narrow rows, most of whose groups would hang over an end.
 struct Walk {
   i64 first;                     // its first tile
@@ -99,7 +99,7 @@ struct Clip {
   int* status;
 };
 
-// A beta in two parts, hi + lo within 2^-48 of it.  Rounded to fp32 alone it is off by as much as the rounding of a state, but the
+// A beta in two parts, hi + lo within 2^-47 of it.  Rounded to fp32 alone it is off by as much as the rounding of a state, but the
 // same way in every step: V would settle 1.7e-4 off for beta2 = 0.9999, 1.4e-3 for 0.99999.  lo is above zero (unless beta is zero),
 // so that an infinite state stays infinite.
 struct Beta {
@@ -266,7 +266,7 @@ __device__ __forceinline__ Spot spot_in(const Walk& w, const RowRun& r, i64 k) {
   return s;
 }
 
-// Sums in 64 bits: squares of fp32 values neither overflow nor vanish there.  A group's squares are added in fp32 first (a
+// Sums in 64 bits: squares of fp32 values neither overflow nor vanish there.  A group's eight squares are added in fp32 first (a
 // conversion and a 64-bit operation per element would cost more than the memory: 436M x 4 bf16 elements 6566 us); a sum that left
 // fp32's range, or came close enough to its lower end to have lost something, is taken again.  Maxima on the magnitudes'
 // bits, whose order is that of the values with NaN above infinity, so that a NaN is never lost.
@@ -690,7 +690,8 @@ __global__ void __launch_bounds__(THREADS, SCALE_RESIDENT) k_list_scale(const __
   // What the norm's launch read last is still in L2: a block of one wave has the tiles that it had there and walks them from the
   // end; of many blocks those at the list's end come first.
   const i64 b = gridDim.x - 1 - blockIdx.x, t0 = first_tile(t, b), t1 = first_tile(t, b + 1);
-  // (The search and, further down, the first loads do not wait for the coefficient, except where it may say that nothing is to be done.)
+  // (The search does not wait for the launch in front, except where the coefficient may say that nothing is to be done.  The loads of
+  // G come behind the coefficient: where it is made of a norm's sums or of given norms, behind that reduction's barriers and shuffles.)
   i64 i = !c.in_place && t0 < t1 ? find_item(t, t1 - 1) : 0;
   pdl_enter();
   float coef;
