@@ -452,7 +452,7 @@ class Dion:
     def adamw_step(self, params: ParamList, lr: float, step, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8,
                    grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
         """One AdamW step on a list.  step: its number t, from 1, or an int64 CUDA tensor that holds it.  grad_scale: the
-        factor of the gradients on the device (a clipping coefficient)."""
+        factor of the gradients on the device (a clipping coefficient).  eps: 0, or from 2^-126 to 2^125."""
         items = self._items(params, ParamList)
         if isinstance(step, torch.Tensor):
             if step.get_device() != self.device or step.dtype != torch.int64 or step.numel() != 1:

@@ -100,8 +100,8 @@ struct Clip {
 };
 
 // A beta in two parts, hi + lo within 2^-47 of it.  Rounded to fp32 alone it is off by as much as the rounding of a state, but the
-// same way in every step: V would settle 1.7e-4 off for beta2 = 0.9999, 1.4e-3 for 0.99999.  lo is above zero (unless beta is zero),
-// so that an infinite state stays infinite.
+// same way in every step: V would settle 1.7e-4 off for beta2 = 0.9999, 1.4e-3 for 0.99999.  lo is above zero (unless beta is zero or
+// next to it), so that an infinite state stays infinite.
 struct Beta {
   float hi, lo;
 };
